@@ -51,12 +51,12 @@ extern "C" {
 typedef enum {
     LORA_OK = 0,
     LORA_ERR_NULL = 1,        /* a required pointer is NULL */
-    LORA_ERR_SHAPE = 2,       /* negative size, or K/N == 0, or M >= 2^31 */
+    LORA_ERR_SHAPE = 2,       /* negative size, or K/N == 0, or M >= 2^31; a stride that does not fit its heads */
     LORA_ERR_ALIGN = 3,       /* a device pointer is not 16-byte aligned */
-    LORA_ERR_PARAM = 4,       /* p outside [0,1), or p/s not finite */
+    LORA_ERR_PARAM = 4,       /* p outside [0,1), or p/s not finite; eps or scale not positive and finite */
     LORA_ERR_SEGMENTS = 5,    /* offsets do not rise from 0 to M */
-    LORA_ERR_WORKSPACE = 6,   /* workspace smaller than lora_bwd_workspace_bytes(); lora_bwd_noalloc: beyond its scratch */
-    LORA_ERR_UNSUPPORTED = 7, /* K or N not a multiple of 64 or above 2^22, r not in {16,32,64}, G > 64 */
+    LORA_ERR_WORKSPACE = 6,   /* workspace smaller than the call's ..._workspace_bytes(); lora_bwd_noalloc: beyond its scratch */
+    LORA_ERR_UNSUPPORTED = 7, /* K or N not a multiple of 64 or above 2^22, r not in {16,32,64}, G > 64; heads and pages: see the call */
     LORA_ERR_HIP = 8          /* a kernel launch failed */
 } lora_status;
 
@@ -285,6 +285,83 @@ lora_status lora_ceiling_mfma(const lora_bf16* operands, float* sink, int32_t wo
                               int32_t shape, double* flops, lora_stream stream);
 lora_status lora_ceiling_hbm_read(const void* src, size_t bytes, uint32_t* sink, int32_t workgroups,
                                   lora_stream stream);
+
+/* ---- Serving adapters, and what stands behind the query and key projections ------------------------
+ *
+ * Once trained, adapters are served: a step holds the rows of many requests, each with its own adapter, then the attention of
+ * their new tokens over a cache of keys and values.  The same conventions as above; "device arrays" are read by the kernels, so their
+ * values are not checked on the host, and what is out of range in them is handled as each call says.  Strides (ld*) are the
+ * distances of rows in elements, multiples of 8, the heads of a row lying side by side.  fp32 inside; outputs rounded once. */
+
+/* Forward of a batch in which every row names its adapter:
+ *   Y[i] = X[i] W^T + s[g] (X[i] A[g]^T) B[g]^T,   g = ids[i];  a row with ids[i] outside 0 .. P-1 has no adapter.
+ * X [M,K]  W [N,K]  A [P,r,K]  B [P,N,r]  Y [M,N];  device arrays ids [M], s [P], ranks [P].  ranks (may be NULL: all r): adapter g
+ * uses the first ranks[g] rows of A[g] and columns of B[g], any number of 0 .. r (values outside are cut to it); the others may
+ * hold anything.  S [M,r]: scratch that receives s (X A^T), zero past the rank.  No dropout: a row's result is that of lora_fwd
+ * with p = 0 up to rounding of S.  M < 2^31, K, N, r as above; any P >= 1; adapters may come in any order and number. */
+lora_status lora_requests_fwd(const lora_bf16* X, const lora_bf16* W, const lora_bf16* A, const lora_bf16* B, const int32_t* ids,
+                              const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P, lora_bf16* Y,
+                              lora_bf16* S, lora_stream stream);
+
+/* RMS norm of every query and key head and rotation by the row's position, one pass:
+ *   n = x / sqrt(mean(x^2) + eps);  y = R(gamma n)
+ * for the H query heads and G key heads (D entries each) of M rows; gamma_q, gamma_k [D].  R turns the pairs (i, i + rot/2), or with
+ * interleaved != 0 (2i, 2i+1), of the first rot entries by the angle whose cosine and sine stand in row pos[row] of cos_table,
+ * sin_table [positions, rot/2] (fp32); pos [M] is a device array.  A row whose position is outside the tables gets zeros.
+ * D: multiples of 16 up to 256; rot: multiples of 16 up to D; H, G up to 1024; M < 2^26; eps > 0.  The output may be the input. */
+lora_status lora_qk_norm_rope_fwd(const lora_bf16* q, const lora_bf16* k, const lora_bf16* gamma_q, const lora_bf16* gamma_k,
+                                  const float* cos_table, const float* sin_table, const int32_t* pos, int64_t M, int32_t H, int32_t G, int32_t D,
+                                  int32_t rot, int64_t positions, int64_t ldq, int64_t ldk, int64_t ldqo, int64_t ldko, float eps,
+                                  int interleaved, lora_bf16* q_out, lora_bf16* k_out, lora_stream stream);
+
+/* Its backward: dq, dk from dq_out, dk_out and the forward's inputs; dgamma_q, dgamma_k [D] fp32, overwritten or, with accumulate != 0,
+ * added to (rows whose position is outside the tables add nothing; M = 0 leaves them at zero).  workspace: device scratch of at least
+ * lora_qk_norm_rope_workspace_bytes(), 256-byte aligned.  The same inputs give the same bits. */
+size_t lora_qk_norm_rope_workspace_bytes(int64_t M, int32_t H, int32_t G, int32_t D);
+lora_status lora_qk_norm_rope_bwd(const lora_bf16* q, const lora_bf16* k, const lora_bf16* gamma_q, const lora_bf16* gamma_k,
+                                  const float* cos_table, const float* sin_table, const int32_t* pos, const lora_bf16* dq_out,
+                                  const lora_bf16* dk_out, int64_t M, int32_t H, int32_t G, int32_t D, int32_t rot, int64_t positions, int64_t ldq,
+                                  int64_t ldk, int64_t lddqo, int64_t lddko, int64_t lddq, int64_t lddk, float eps, int interleaved, lora_bf16* dq,
+                                  lora_bf16* dk, float* dgamma_q, float* dgamma_k, int accumulate, void* workspace, size_t workspace_bytes,
+                                  lora_stream stream);
+
+/* A paged cache of keys and values (the caller's device memory): k, v [pages, heads, page, dim].  fp8 == 0: lora_bf16.  fp8 != 0: e4m3
+ * bytes, and k_exp, v_exp [pages, heads, page] with the biased exponent of one power of two for every token and head; the value is
+ * e4m3 * 2^(exp - 127).  page: a power of two, 16 .. 1024 tokens; dim: multiples of 16 up to 256; heads up to 1024. */
+typedef struct {
+    void* k;
+    void* v;
+    uint8_t* k_exp;
+    uint8_t* v_exp;
+    int64_t pages;
+    int32_t page, heads, dim, fp8;
+} lora_kv_cache;
+
+/* Writes row i of k and v [M, heads, dim] to slot slots[i] = page number * page + place in it (device array; a slot outside the cache
+ * is left out; slots of one call must differ, or one of the rows is kept, not always the same one).  fp8: the power of two is the
+ * smallest (2^-117 at least, 1 for a head of zeros) that keeps the head's largest finite magnitude within 448; values are rounded to
+ * nearest even, what is not finite becomes NaN. */
+lora_status lora_kv_cache_write(const lora_kv_cache* cache, const lora_bf16* k, const lora_bf16* v, int64_t ldk, int64_t ldv, const int64_t* slots,
+                                int64_t M, lora_stream stream);
+/* ... and reads slots back, exactly; a slot outside the cache reads as zeros. */
+lora_status lora_kv_cache_read(const lora_kv_cache* cache, const int64_t* slots, int64_t M, lora_bf16* k, lora_bf16* v, int64_t ldk, int64_t ldv,
+                               lora_stream stream);
+
+/* Attention of new tokens over a paged cache that holds them already.  q, out [T, H, dim]: the new tokens of B sequences end to end,
+ * sequence b's being rows offsets[b] .. offsets[b+1]-1; with kv_lens[b] tokens in the cache, the last of them the new ones; its token j
+ * is row j % page of page table[b * ldt + j / page].  The new token at position pos sees the keys j <= pos and, with window > 0, only
+ * j > pos - window; query head h uses key/value head h / (H / heads).
+ *   out = sum_j softmax_j(scale q k_j) v_j;   a row that sees no key (fewer keys than new tokens): zeros.
+ * offsets [B+1], kv_lens [B] and table are device arrays; max_new and max_kv (host) are the largest number of new tokens and the largest
+ * length: rows past max_new of a sequence are not computed, and a larger length than max_kv costs time only.  Lengths are cut to max_pages
+ * pages and page numbers to the cache.  Cache entries past a sequence's length may hold anything; keys that only
+ * some rows of a chunk see must be finite.  dim 64 or 128; T * H < 2^31; lengths below 2^30.  workspace: device scratch of at
+ * least lora_paged_attn_workspace_bytes(), 256-byte aligned.  The same inputs and sizes give the same bits. */
+size_t lora_paged_attn_workspace_bytes(const lora_kv_cache* cache, int64_t T, int32_t H, int64_t B, int64_t max_new, int64_t max_kv, int32_t window);
+lora_status lora_paged_attn_fwd(const lora_bf16* q, const lora_kv_cache* cache, const int32_t* table, const int32_t* offsets, const int32_t* kv_lens,
+                                int64_t T, int32_t H, int64_t B, int64_t max_pages, int64_t ldq, int64_t ldt, int64_t ldo, int64_t max_new,
+                                int64_t max_kv, float scale, int32_t window, lora_bf16* out, void* workspace, size_t workspace_bytes,
+                                lora_stream stream);
 
 const char* lora_status_string(lora_status st);
 int lora_version(void);

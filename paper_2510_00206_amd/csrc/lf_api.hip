@@ -451,10 +451,10 @@ const char* lora_status_string(lora_status st) {
         case LORA_ERR_NULL: return "a required pointer is NULL";
         case LORA_ERR_SHAPE: return "invalid shape";
         case LORA_ERR_ALIGN: return "pointer not sufficiently aligned";
-        case LORA_ERR_PARAM: return "dropout probability outside [0,1) or non-finite scale";
+        case LORA_ERR_PARAM: return "dropout probability outside [0,1), non-finite scale, or eps or scale of scores not positive";
         case LORA_ERR_SEGMENTS: return "segment offsets must rise from 0 to M";
         case LORA_ERR_WORKSPACE: return "workspace too small (lora_bwd_noalloc: problem beyond the built-in scratch)";
-        case LORA_ERR_UNSUPPORTED: return "unsupported size (K, N multiples of 64; r in {16,32,64}; G <= 64)";
+        case LORA_ERR_UNSUPPORTED: return "unsupported size (K, N multiples of 64; r in {16,32,64}; G <= 64; heads and pages: see the header)";
         case LORA_ERR_HIP: return "kernel launch failed";
     }
     return "unknown status";

@@ -1044,7 +1044,8 @@ static double launch_cost(const TileCost& c, int64_t tiles, int64_t slabs, int a
 struct GemmPart { int kind, row_lo, row_hi; int64_t tiles_m; };
 struct GemmPlan { int uniform, parts; GemmPart part[2]; };
 
-static GemmPlan plan_gemm(const AdapterTable& tb, int M, int kc, int nc, int r, int forced) {
+// `small`: of the small tiles only
+static GemmPlan plan_gemm(const AdapterTable& tb, int M, int kc, int nc, int r, int forced, bool small = false) {
     GemmPlan best{tb.G > 1 && boundaries_on_64(tb), 0, {}};
     if (M == 0) return best;
     const int64_t slabs = kc / BK + (r > 0);
@@ -1057,7 +1058,7 @@ static GemmPlan plan_gemm(const AdapterTable& tb, int M, int kc, int nc, int r, 
     auto cost_of = [&](int kind, int64_t tiles) { return launch_cost(kind < 0 ? kLargeCost[-1 - kind] : kRingCost[kind], tiles, slabs, tb.G); };
     const int only = forced == 256 ? -1 : 0;         // (the knob fixes the 256-row tiles, or 128 x 256)
     double cost = 1e30;
-    for (int k = forced ? only : -kLargeKinds; k < (forced ? only + 1 : kRingKinds); ++k) {
+    for (int k = forced ? only : small ? 0 : -kLargeKinds; k < (forced ? only + 1 : kRingKinds); ++k) {
         const int64_t tm = tiles_of(k, 0), tn = columns(k);
         const double all = cost_of(k, tm * tn);
         if (all < cost) {
@@ -1092,6 +1093,19 @@ int gemm_tiles(const AdapterTable& tb, int M, int contraction, int columns, int 
         const int k = t.part[i].kind;
         out[i] = k < 0 ? GemmTile{kLargeRows[-1 - k], BN, t.part[i].row_lo}
                        : GemmTile{kRingTiles[k][0], kRingTiles[k][1], t.part[i].row_lo};
+    }
+    return t.parts;
+}
+
+int plan_ring(int M, int contraction, int columns, RingPart (&out)[2]) {
+    AdapterTable tb;
+    memset(&tb, 0, sizeof(tb));
+    tb.G = 1;
+    tb.row0[1] = M;
+    const GemmPlan t = plan_gemm(tb, M, contraction, columns, 0, 0, true);
+    for (int i = 0; i < t.parts; ++i) {
+        const int k = t.part[i].kind;
+        out[i] = RingPart{k, t.part[i].row_lo, t.part[i].row_hi, (int)t.part[i].tiles_m, (columns + kRingTiles[k][1] - 1) / kRingTiles[k][1]};
     }
     return t.parts;
 }

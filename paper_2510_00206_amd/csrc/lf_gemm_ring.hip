@@ -293,6 +293,61 @@ __device__ __forceinline__ void ring_stage(f32x4 (&acc)[C::MI][C::NI], const Rin
     }
 }
 
+// LoRA term of rows with an adapter each, on the accumulators of the wave's MI x NI blocks: one matrix step (two at rank 64) for every
+// adapter among its rows, with the other rows' S left out, so that no value of one adapter meets a row of another, not even multiplied
+// by zero.  S and B come straight from memory in the fragments' layout: an adapter's few rows are read once, and by this wave alone.
+template <class C>
+__device__ __forceinline__ void request_term(const RingRequestArgs& p, f32x4 (&acc)[C::MI][C::NI], const RowTile& rt, int c0, int wm, int wn) {
+    const int l = threadIdx.x & 63;
+    int id[C::MI];
+    uint32_t todo[C::MI], any = 0;                           // rows (bits) of a block whose adapter is still to come
+#pragma unroll
+    for (int mi = 0; mi < C::MI; ++mi) {
+        const int row = (wm * C::MI + mi) * 16 + (l & 15);
+        id[mi] = p.ids[rt.row_start + min(row, rt.rows - 1)];
+        if (row >= rt.rows || id[mi] >= p.P) id[mi] = -1;
+        todo[mi] = (uint32_t)__ballot(id[mi] >= 0) & 0xFFFFu;
+        any |= todo[mi];
+    }
+    const lora_bf16* brow[C::NI];
+#pragma unroll
+    for (int ni = 0; ni < C::NI; ++ni) brow[ni] = p.lout + (int64_t)min(c0 + (wn * C::NI + ni) * 16 + (l & 15), p.NC - 1) * p.lr;
+    while (any) {
+        int g = -1;
+        any = 0;
+#pragma unroll
+        for (int mi = 0; mi < C::MI; ++mi) {
+            if (g < 0 && todo[mi]) g = __builtin_amdgcn_readlane(id[mi], __builtin_ctz(todo[mi]));
+            todo[mi] &= ~(uint32_t)__ballot(id[mi] == g);
+            any |= todo[mi];
+        }
+        const int rank = p.ranks ? min(p.ranks[g], p.lr) : p.lr;
+        for (int kk = 0; kk * 32 < rank; ++kk) {
+            const int k = 32 * kk + 8 * (l >> 4), left = rank - k;      // entries of this lane's eight that the adapter has
+            u32x4 b[C::NI];
+#pragma unroll
+            for (int ni = 0; ni < C::NI; ++ni) {
+                b[ni] = u32x4{0u, 0u, 0u, 0u};
+                if (left > 0) b[ni] = *(const u32x4*)(brow[ni] + (int64_t)g * p.NC * p.lr + k);
+            }
+            if (left > 0 && left < 8)
+#pragma unroll
+                for (int ni = 0; ni < C::NI; ++ni)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) b[ni][i] &= 2 * i + 1 < left ? 0xFFFFFFFFu : 2 * i < left ? 0xFFFFu : 0u;
+#pragma unroll
+            for (int mi = 0; mi < C::MI; ++mi) {
+                if (__ballot(id[mi] == g) == 0) continue;
+                u32x4 s = u32x4{0u, 0u, 0u, 0u};
+                if (left > 0 && id[mi] == g) s = *(const u32x4*)(p.ltok + (int64_t)(rt.row_start + (wm * C::MI + mi) * 16 + (l & 15)) * p.lr + k);
+#pragma unroll
+                for (int ni = 0; ni < C::NI; ++ni)
+                    acc[mi][ni] = LF_MFMA(__builtin_bit_cast(bf16x8, b[ni]), __builtin_bit_cast(bf16x8, s), acc[mi][ni]);
+            }
+        }
+    }
+}
+
 template <class C, bool COL, class Args>
 __device__ __forceinline__ void ring_tile(const Args& p, char* smem) {
     constexpr int NS = C::NS, MI = C::MI, NI = C::NI;
@@ -412,7 +467,10 @@ __device__ __forceinline__ void ring_tile(const Args& p, char* smem) {
 
     // LoRA term: (2) on the same accumulators; (5) by itself, masked and added
     const int rank_chunks = has_lora ? p.tb.a[rt.g].rank >> 3 : 0;
-    if (has_lora) {
+    if constexpr (std::is_same_v<Args, RingRequestArgs>) {
+        ring_mfma_done<MI, NI>(acc);
+        request_term<C>(p, acc, rt, c0, wm, wn);
+    } else if (has_lora) {
         // block rows of the tile from row `first` on into `to`; the fragments of sub-step 0 are in f0
         auto term = [&](auto& to, auto first) {
             constexpr int FIRST = first(), ROWS = sizeof(to) / sizeof(to[0]);
@@ -495,6 +553,12 @@ __global__ void __launch_bounds__(C::THREADS + 64 * C::CW) ring_gemm_kernel(Ring
     ring_tile<C, COL>(p, smem);
 }
 
+template <class C>
+__global__ void __launch_bounds__(C::THREADS + 64 * C::CW) ring_requests_kernel(RingRequestArgs p) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    ring_tile<C, false>(p, smem);
+}
+
 // (5) and the strips of (4) and dB, neither of which needs the other, in one launch of DA_THREADS a workgroup (rule and figures at
 // kStripsBeside); the waves that a tile has no work for end at once.  Bounded by the latency of one sweep over the contraction.
 template <class C, int CB, class TB>
@@ -572,8 +636,8 @@ constexpr int kLongContraction = 4096;
 constexpr bool deep_stages(int KC, int NC, int64_t tiles) { return KC >= 1024 && NC % 256 == 0 && tiles <= 2 * kComputeUnits; }
 
 // Calls f(kernel, arguments) with what a launch of tiles of `kind` takes.
-template <bool COL, class F>
-static auto with_ring(int kind, const RingArgs& a, F&& f) {
+template <bool COL, class Args, class F>
+static auto with_ring(int kind, const Args& a, F&& f) {
     switch (kind) {
         case 0: return f(Ring<128, 256, 2, 4, 3, 0, 4>{}, a);
         case 1: return f(Ring<128, 128, 2, 2, 4, 2, 2>{}, a);
@@ -581,7 +645,7 @@ static auto with_ring(int kind, const RingArgs& a, F&& f) {
         case 3: return f(Ring<64, 64, 2, 2, COL ? 4 : 5, 2, 2>{}, a);
         case 4:
             if (ring_halves(a.tiles_m, a.tiles_n)) {
-                RingArgs h = a;
+                Args h = a;
                 h.tiles_n *= 2;
                 return f(Ring32x32{}, h);
             }
@@ -626,6 +690,22 @@ static hipError_t launch_ring_dir(int kind, const RingArgs& a, hipStream_t st) {
 
 hipError_t launch_ring(int kind, bool col, const RingArgs& a, hipStream_t st) {
     return col ? launch_ring_dir<true>(kind, a, st) : launch_ring_dir<false>(kind, a, st);
+}
+
+template <class C>
+static hipError_t launch_requests_cfg(const RingRequestArgs& a, hipStream_t st) {
+    static bool attr_set = false;                  // one flag per instantiation
+    if (!attr_set) {
+        hipError_t e = hipFuncSetAttribute((const void*)ring_requests_kernel<C>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+        if (e != hipSuccess) return e;
+        attr_set = true;
+    }
+    hipLaunchKernelGGL(ring_requests_kernel<C>, dim3((unsigned)((int64_t)a.tiles_m * a.tiles_n)), dim3(C::THREADS + 64 * C::CW), C::LDS, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_ring_requests(int kind, const RingRequestArgs& a, hipStream_t st) {
+    return with_ring<false>(kind, a, [&](auto c, const RingRequestArgs& b) { return launch_requests_cfg<decltype(c)>(b, st); });
 }
 
 hipError_t launch_ring_strips(int kind, const RingStripsArgs& a, hipStream_t st) {

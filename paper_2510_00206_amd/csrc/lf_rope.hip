@@ -1,0 +1,293 @@
+// Norms of queries and keys for each head with the rotation by the row's position in the same pass, and its backward.
+//   forward    n = x / rms,  rms = sqrt(mean(x^2) + eps);  y = R(gamma n)
+//   backward   e = R^T dy;  dgamma = sum e n;  u = gamma e;  dx = (u - n mean(u n)) / rms
+// R turns pairs of the head's first `rot` entries by the angles of its position.  x is read once (backward: x and dy), statistics are
+// fp32, the result is rounded once.  Bound by HBM: 4 (6) bytes an element.  Eight entries to a lane (16-byte loads), 8, 16 or
+// 32 lanes to a head by its size; a head's sums are butterflies over its lanes.  With R's cosines and sines multiplied by gamma once per
+// row, y is one product and one multiply-add an entry; a pair's other entry comes from the lane that holds it, as the bf16 it was.
+#include "lf_serve.h"
+
+namespace lf {
+
+constexpr int kRopeThreads = 256;
+
+// GL lanes to a head, a wave for a row, or for a part of its heads.
+template <int GL, bool INTER>
+struct RopeLane {
+    int j, slot;                       // lane of the head, head of the wave
+    bool active, turned;               // ... has entries; they are in the rotated part
+    int at, other;                     // first index into a row of the tables; wave lane with the other entries of this one's pairs
+    float sign;                        // of the sine in y: - for the first entry of a pair
+    __device__ __forceinline__ RopeLane(int D, int rot) {
+        const int l = threadIdx.x & 63;
+        j = l % GL;
+        slot = l / GL;
+        active = 8 * j < D;
+        turned = 8 * j < rot;
+        const bool first = INTER || 8 * j < rot / 2;
+        at = INTER ? 4 * j : first ? 8 * j : 8 * j - rot / 2;
+        other = INTER || !turned ? l : first ? l + rot / 16 : l - rot / 16;
+        sign = first ? -1.f : 1.f;
+    }
+};
+
+template <int GL>
+__device__ __forceinline__ float sum_over_head(float v) {
+#pragma unroll
+    for (int o = GL / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// Cosine and (signed) sine of each of a lane's entries.
+template <int GL, bool INTER>
+__device__ __forceinline__ void angles(const RopeArgs& p, const RopeLane<GL, INTER>& ln, int pos, bool known, float (&c)[8], float (&s)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { c[i] = 1.f; s[i] = 0.f; }
+    if (!ln.turned || !known) return;
+    const float* cr = p.cos_ + (int64_t)pos * (p.rot / 2) + ln.at;
+    const float* sr = p.sin_ + (int64_t)pos * (p.rot / 2) + ln.at;
+    if constexpr (INTER) {
+        const f32x4 cv = *(const f32x4*)cr, sv = *(const f32x4*)sr;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { c[i] = cv[i / 2]; s[i] = i & 1 ? sv[i / 2] : -sv[i / 2]; }
+    } else {
+        const f32x4 c0 = *(const f32x4*)cr, c1 = *(const f32x4*)(cr + 4), s0 = *(const f32x4*)sr, s1 = *(const f32x4*)(sr + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { c[i] = i < 4 ? c0[i & 3] : c1[i & 3]; s[i] = ln.sign * (i < 4 ? s0[i & 3] : s1[i & 3]); }
+    }
+}
+
+// The other entries of this lane's pairs.
+template <int GL, bool INTER>
+__device__ __forceinline__ void others(const RopeLane<GL, INTER>& ln, u32x4 raw, float (&o)[8]) {
+    if constexpr (INTER) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = raw[i] >> 16 | raw[i] << 16;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = __shfl(raw[i], ln.other);
+    }
+    unpack8(raw, o);
+}
+
+template <int GL, bool INTER>
+__device__ __forceinline__ void gamma_of(const lora_bf16* g, const RopeLane<GL, INTER>& ln, float (&own)[8]) {
+    u32x4 v = u32x4{0u, 0u, 0u, 0u};
+    if (ln.active) v = *(const u32x4*)(g + 8 * ln.j);
+    unpack8(v, own);
+}
+
+// A wave's row is done in passes of 64 / GL heads, first the queries' passes, then the keys'; part i of the row takes passes i, i + parts, ..
+template <int GL>
+struct RopePasses {
+    static constexpr int HEADS = 64 / GL;
+    int of_q, all;
+    __host__ __device__ RopePasses(int H, int G) : of_q((H + HEADS - 1) / HEADS), all((H + HEADS - 1) / HEADS + (G + HEADS - 1) / HEADS) {}
+};
+
+template <int GL, bool INTER>
+__global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
+    const int64_t unit = (int64_t)blockIdx.x * (kRopeThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row = unit / p.parts;
+    if (row >= p.M) return;
+    const RopeLane<GL, INTER> ln(p.D, p.rot);
+    const RopePasses<GL> ps(p.H, p.G);
+    const int pos = p.pos[row];
+    const bool known = pos >= 0 && pos < p.positions;
+    float cq[8], sq[8], ck[8], sk[8];
+    {
+        float c[8], s[8], g[8], o[8];
+        angles(p, ln, pos, known, c, s);
+        auto fold = [&](const lora_bf16* gamma, float (&cg)[8], float (&sg)[8]) {
+            gamma_of(gamma, ln, g);
+            others(ln, pack8(g), o);                       // (gamma is bf16: packing it again is exact)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { cg[i] = c[i] * g[i]; sg[i] = s[i] * o[i]; }
+        };
+        fold(p.gamma_q, cq, sq);
+        fold(p.gamma_k, ck, sk);
+    }
+    constexpr int U = 4;                                   // passes whose loads are in flight together
+    for (int first = (int)(unit % p.parts); first < ps.all; first += U * p.parts) {
+        u32x4 raw[U];
+        bool ok[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int pass = first + u * p.parts;
+            const bool is_q = pass < ps.of_q;
+            const int head = (is_q ? pass : pass - ps.of_q) * ps.HEADS + ln.slot;
+            ok[u] = pass < ps.all && ln.active && head < (is_q ? p.H : p.G);
+            raw[u] = u32x4{0u, 0u, 0u, 0u};
+            if (ok[u]) raw[u] = *(const u32x4*)((is_q ? p.q + row * p.ldq : p.k + row * p.ldk) + (int64_t)head * p.D + 8 * ln.j);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int pass = first + u * p.parts;
+            if (pass >= ps.all) break;
+            const bool is_q = pass < ps.of_q;
+            const int head = (is_q ? pass : pass - ps.of_q) * ps.HEADS + ln.slot;
+            float x[8], o[8], y[8], sum = 0.f;
+            unpack8(raw[u], x);
+            others(ln, raw[u], o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
+            const float inv = 1.f / sqrtf(sum_over_head<GL>(sum) / (float)p.D + p.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = inv * (x[i] * (is_q ? cq[i] : ck[i]) + o[i] * (is_q ? sq[i] : sk[i]));
+            u32x4 out = pack8(y);
+            if (!known) out = u32x4{0u, 0u, 0u, 0u};
+            if (ok[u]) *(u32x4*)((is_q ? p.q_out + row * p.ldqo : p.k_out + row * p.ldko) + (int64_t)head * p.D + 8 * ln.j) = out;
+        }
+    }
+}
+
+template <int GL, bool INTER>
+__global__ void __launch_bounds__(kRopeThreads) rope_bwd_kernel(RopeArgs p) {
+    __shared__ float red[kRopeThreads / 64][2][GL * 8];
+    const RopeLane<GL, INTER> ln(p.D, p.rot);
+    const RopePasses<GL> ps(p.H, p.G);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    float gq[8], gk[8], dgq[8], dgk[8];
+    gamma_of(p.gamma_q, ln, gq);
+    gamma_of(p.gamma_k, ln, gk);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dgq[i] = dgk[i] = 0.f;
+    const int64_t units = p.M * p.parts;
+    for (int64_t unit = (int64_t)blockIdx.x * (kRopeThreads / 64) + w; unit < units; unit += (int64_t)gridDim.x * (kRopeThreads / 64)) {
+        const int64_t row = unit / p.parts;
+        const int pos = p.pos[row];
+        const bool known = pos >= 0 && pos < p.positions;
+        float c[8], s[8];
+        angles(p, ln, pos, known, c, s);
+        constexpr int U = 2;
+        for (int first = (int)(unit % p.parts); first < ps.all; first += U * p.parts) {
+            u32x4 xr[U], dr[U];
+            bool ok[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int pass = first + u * p.parts;
+                const bool is_q = pass < ps.of_q;
+                const int head = (is_q ? pass : pass - ps.of_q) * ps.HEADS + ln.slot;
+                ok[u] = pass < ps.all && ln.active && head < (is_q ? p.H : p.G);
+                xr[u] = dr[u] = u32x4{0u, 0u, 0u, 0u};
+                if (ok[u]) {
+                    xr[u] = *(const u32x4*)((is_q ? p.q + row * p.ldq : p.k + row * p.ldk) + (int64_t)head * p.D + 8 * ln.j);
+                    if (known) dr[u] = *(const u32x4*)((is_q ? p.dq_out + row * p.lddq : p.dk_out + row * p.lddk) + (int64_t)head * p.D + 8 * ln.j);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int pass = first + u * p.parts;
+                if (pass >= ps.all) break;
+                const bool is_q = pass < ps.of_q;
+                const int head = (is_q ? pass : pass - ps.of_q) * ps.HEADS + ln.slot;
+                float x[8], e[8], o[8], sxx = 0.f, sux = 0.f;
+                unpack8(xr[u], x);
+                unpack8(dr[u], e);
+                others(ln, dr[u], o);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    e[i] = e[i] * c[i] - o[i] * s[i];
+                    sxx += x[i] * x[i];
+                    sux += e[i] * (is_q ? gq[i] : gk[i]) * x[i];
+                }
+                sxx = sum_over_head<GL>(sxx);
+                sux = sum_over_head<GL>(sux);
+                const float inv = 1.f / sqrtf(sxx / (float)p.D + p.eps), back = inv * inv * sux / (float)p.D;
+                float dx[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float n = e[i] * x[i] * inv;
+                    if (is_q) dgq[i] += n;
+                    else dgk[i] += n;
+                    dx[i] = inv * (e[i] * (is_q ? gq[i] : gk[i]) - x[i] * back);
+                }
+                u32x4 out = pack8(dx);
+                if (!known) out = u32x4{0u, 0u, 0u, 0u};
+                if (ok[u]) *(u32x4*)((is_q ? p.q_out + row * p.ldqo : p.k_out + row * p.ldko) + (int64_t)head * p.D + 8 * ln.j) = out;
+            }
+        }
+    }
+    // over the heads of the wave, then over the waves, in a fixed order
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int o = GL; o < 64; o <<= 1) {
+            dgq[i] += __shfl_xor(dgq[i], o);
+            dgk[i] += __shfl_xor(dgk[i], o);
+        }
+        if (ln.slot == 0) {
+            red[w][0][8 * ln.j + i] = dgq[i];
+            red[w][1][8 * ln.j + i] = dgk[i];
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * p.D; i += kRopeThreads) {
+        const int t = i >= p.D, d = i - t * p.D;
+        p.part[(int64_t)blockIdx.x * 2 * p.D + i] = ((red[0][t][d] + red[1][t][d]) + red[2][t][d]) + red[3][t][d];
+    }
+}
+
+// dgamma (+)= the sum over the blocks' planes: 16 columns to a workgroup, 16 threads to a column, each with every 16th plane.
+__global__ void __launch_bounds__(256) rope_finalize_kernel(RopeFinalizeArgs p) {
+    __shared__ float red[16][17];
+    const int cl = threadIdx.x & 15, sl = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
+    float v = 0.f;
+    for (int b = sl; b < p.blocks; b += 16) v += p.part[(int64_t)b * 2 * p.D + c];
+    red[sl][cl] = v;
+    __syncthreads();
+    if (sl) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v += red[i][cl];
+    float* out = c < p.D ? p.dgamma_q + c : p.dgamma_k + c - p.D;
+    *out = p.accumulate ? *out + v : v;
+}
+
+// Parts of a row while there are fewer rows than 16 waves to a compute unit, but no more than its passes.
+template <int GL>
+static int rope_parts(int64_t M, int H, int G) {
+    const int all = RopePasses<GL>(H, G).all;
+    const int64_t want = (16 * kComputeUnits + M - 1) / (M > 0 ? M : 1);
+    return (int)(want < all ? want : all);
+}
+template <class F>
+static auto with_lanes(int D, F&& f) {
+    if (D <= 64) return f(std::integral_constant<int, 8>{});
+    if (D <= 128) return f(std::integral_constant<int, 16>{});
+    return f(std::integral_constant<int, 32>{});
+}
+
+hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st) {
+    return with_lanes(a.D, [&](auto gl) {
+        a.parts = rope_parts<gl()>(a.M, a.H, a.G);
+        const int64_t blocks = (a.M * a.parts + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
+        if (interleaved) hipLaunchKernelGGL((rope_fwd_kernel<gl(), true>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
+        else hipLaunchKernelGGL((rope_fwd_kernel<gl(), false>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
+        return hipGetLastError();
+    });
+}
+
+// Every block leaves a plane of partial sums, so no more of them than fill the chip.
+constexpr int kRopeBlocks = 4 * kComputeUnits;
+int rope_blocks(int64_t M, int H, int G, int D) {
+    return with_lanes(D, [&](auto gl) {
+        const int64_t n = (M * rope_parts<gl()>(M, H, G) + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
+        return (int)(n < kRopeBlocks ? n : kRopeBlocks);
+    });
+}
+
+hipError_t launch_rope_bwd(RopeArgs a, bool interleaved, const RopeFinalizeArgs& f, hipStream_t st) {
+    if (f.blocks > 0) {
+        const hipError_t e = with_lanes(a.D, [&](auto gl) {
+            a.parts = rope_parts<gl()>(a.M, a.H, a.G);
+            if (interleaved) hipLaunchKernelGGL((rope_bwd_kernel<gl(), true>), dim3(f.blocks), dim3(kRopeThreads), 0, st, a);
+            else hipLaunchKernelGGL((rope_bwd_kernel<gl(), false>), dim3(f.blocks), dim3(kRopeThreads), 0, st, a);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(rope_finalize_kernel, dim3(2 * a.D / 16), dim3(256), 0, st, f);
+    return hipGetLastError();
+}
+
+}  // namespace lf

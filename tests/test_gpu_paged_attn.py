@@ -1,0 +1,177 @@
+"""Attention over the paged cache against the 64-bit form: lengths from one token, ragged batches, every grouping of heads and kernel form, windows,
+rows that see nothing, and anything at all in the cache behind a sequence's end."""
+import pytest
+import torch
+
+from paper_2510_00206_amd import binding
+from serve_util import BF16, F64, attention, gen, normal, quantised, widened, within
+
+pytestmark = pytest.mark.gpu
+NAN = float("nan")
+
+
+def _setup(seqs, H, G, D, page, fp8, seed, junk=True, spare=3, std=1.0):
+    """seqs: [(new, length)].  (q, cache, table, offsets, lens, keys and values of each sequence in 64 bits)"""
+    g = gen(seed)
+    used = [-(-kv // page) for _, kv in seqs]
+    pages = sum(used) + spare
+    width = max(used + [1]) + 2
+    k, v = normal(g, (pages, G, page, D), std), normal(g, (pages, G, page, D))
+    order = torch.randperm(pages, generator=g).to(torch.int32)
+    table = torch.full((len(seqs), width), 1 << 30 if junk else 0, dtype=torch.int32)
+    table[:, 1::2] = -5 if junk else 0
+    at, ends = 0, []
+    for b, (_, kv) in enumerate(seqs):
+        table[b, :used[b]] = order[at:at + used[b]]
+        if kv % page and junk:
+            ends.append((int(order[at + used[b] - 1]), kv % page))
+        at += used[b]
+    ke = ve = None
+    if fp8:
+        # (the exponents are those of each head's magnitude; codes by torch's own conversion, which the cache's tests pin)
+        e = torch.randint(118, 132, (2, pages, G, page), generator=g, dtype=torch.uint8)
+        k, v = (torch.ldexp(x.float(), 127 - y[..., None].int() + 4).clamp(-448, 448).to(torch.float8_e4m3fn) for x, y in zip((k, v), e))
+        ke, ve = e[0].contiguous(), e[1].contiguous()
+        kd, vd = (torch.ldexp(x.to(F64), y[..., None].int() - 127) for x, y in ((k, ke), (v, ve)))
+        kd, vd = kd, vd
+    else:
+        kd, vd = k.to(F64), v.to(F64)
+    for p, o in ends:
+        if fp8:
+            for x in (k, v):
+                x.view(torch.uint8)[p, :, o:] = 0x7F
+        else:
+            k[p, :, o:], v[p, :, o:] = NAN, float("inf")
+    n = [a for a, _ in seqs]
+    q = normal(g, (sum(n), H, D))
+    offsets = torch.tensor([sum(n[:i]) for i in range(len(n) + 1)], dtype=torch.int32)
+    lens = torch.tensor([kv for _, kv in seqs], dtype=torch.int32)
+    held = [tuple(x[table[b, :used[b]].long()].transpose(1, 2).reshape(-1, G, D)[:kv] for x in (kd, vd)) for b, (_, kv) in enumerate(seqs)]
+    cache = binding.KVCache(*(None if t is None else t.cuda() for t in (k, v, ke, ve)))
+    return q, cache, table, offsets, lens, held
+
+
+def _check(seqs, H, G, D, page, fp8, window=0, scale=None, seed=0, max_kv=None, std=1.0):
+    print("attention", seqs[:4], len(seqs), H, G, D, page, fp8, window, flush=True)
+    q, cache, table, offsets, lens, held = _setup(seqs, H, G, D, page, fp8, seed, std=std)
+    out = torch.full(q.shape, 7.0, dtype=BF16, device="cuda")
+    max_new = max([a for a, _ in seqs] + [1])
+    binding.lora_paged_attn_fwd(q.cuda(), cache, table.cuda(), offsets.cuda(), lens.cuda(), max_new, max(max(kv for _, kv in seqs), 1) if max_kv is None else max_kv,
+                                scale=scale, window=window, out=out)
+    torch.cuda.synchronize()
+    at = 0
+    for b, (n, kv) in enumerate(seqs):
+        ref, bound = attention(q[at:at + n].to(F64), *held[b], n, kv, D ** -0.5 if scale is None else scale, window)
+        within(out[at:at + n], ref, bound + 1e-30, (b, n, kv, H, G, D, page, fp8, window))
+        at += n
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("H,G,D,page", [(8, 2, 64, 16), (4, 4, 128, 32), (7, 1, 128, 16), (24, 1, 64, 64), (40, 1, 128, 16), (32, 8, 128, 128)])
+def test_one_token(H, G, D, page, fp8):
+    _check([(1, 1), (1, 2), (1, 15), (1, 16), (1, 17), (1, 33), (1, 100), (1, 257)], H, G, D, page, fp8, seed=H)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("H,G,D,page", [(8, 2, 64, 16), (2, 2, 128, 32), (3, 1, 128, 16), (16, 2, 64, 64), (6, 2, 128, 64)])
+def test_chunks(H, G, D, page, fp8):
+    _check([(1, 1), (5, 5), (7, 200), (64, 64), (33, 150), (70, 301)], H, G, D, page, fp8, seed=H + 1)
+
+
+@pytest.mark.parametrize("n", [2, 8, 9, 16, 17, 31, 32, 33, 127, 128, 129, 200])
+def test_rows_at_the_edges_of_the_tiles(n):
+    _check([(n, n + 41), (n - 1, n + 90)], 2, 2, 64, 16, False, seed=n)
+    _check([(n, n + 41)], 4, 2, 128, 16, True, seed=n)
+
+
+@pytest.mark.parametrize("window", [1, 2, 16, 33, 64, 500, 10 ** 6])
+@pytest.mark.parametrize("seqs", [[(1, 700), (1, 40), (1, 1)], [(5, 300), (9, 9)], [(90, 400), (150, 150)]])
+def test_window(seqs, window):
+    _check(seqs, 8, 2, 64, 16, False, window=window, seed=window)
+    _check(seqs, 4, 2, 128, 32, True, window=window, seed=window)
+
+
+def test_rows_that_see_nothing_and_empty_sequences():
+    """Fewer keys than new tokens: the first of them have no position of their own; sequences without tokens, without keys, without either."""
+    for H, G, D in ((8, 2, 64), (2, 2, 128), (40, 1, 64)):
+        _check([(0, 0), (3, 1), (1, 0), (0, 50), (40, 7), (100, 20), (0, 0)], H, G, D, 16, False)
+        _check([(3, 1), (200, 0), (60, 60)], H, G, D, 16, True, window=5)
+
+
+@pytest.mark.parametrize("seqs,H,G,D,page,fp8", [
+    ([(1, 5000)], 8, 2, 128, 16, True), ([(1, 3001), (1, 20), (1, 1500)], 4, 1, 64, 32, False), ([(4, 4099), (2, 100)], 16, 2, 128, 64, False),
+    ([(70, 3000), (3, 2000)], 4, 2, 64, 16, True), ([(150, 2500)], 2, 1, 128, 16, False)])
+def test_long_ranges_in_parts(seqs, H, G, D, page, fp8):
+    """Ranges that are cut into parts; lengths past max_kv, which sized the parts, cost time only."""
+    q, cache, table, *_ = _setup(seqs, H, G, D, page, fp8, 3)
+    longest, new = max(kv for _, kv in seqs), max(n for n, _ in seqs)
+    assert binding.alloc_paged_attn_workspace(cache, q.shape[0], H, len(seqs), new, longest).numel() > 256
+    _check(seqs, H, G, D, page, fp8, seed=3)
+    _check(seqs, H, G, D, page, fp8, seed=3, max_kv=longest // 3)
+    _check(seqs, H, G, D, page, fp8, seed=3, window=700)
+
+
+def test_peaked_scores_and_scale():
+    """One key takes nearly all of a row, references rise from tile to tile, and a scale other than the default."""
+    _check([(1, 900), (40, 400)], 8, 2, 64, 16, False, scale=1.0, std=3.0, seed=4)
+    _check([(1, 900), (40, 400)], 4, 2, 128, 16, False, scale=0.01, seed=5)
+
+
+def test_inputs_in_a_fused_projection_and_a_wider_table():
+    """q as a part of wider rows, out too, and a table whose rows are apart."""
+    seqs, H, G, D = [(5, 90), (1, 33), (70, 130)], 4, 2, 128
+    q, cache, table, offsets, lens, held = _setup(seqs, H, G, D, 16, False, 8)
+    wide = torch.zeros((q.shape[0], (H + 2 * G) * D), dtype=BF16, device="cuda")
+    wide[:, :H * D] = q.cuda().flatten(1)
+    pages = torch.zeros((len(seqs), table.shape[1] + 5), dtype=torch.int32, device="cuda")
+    pages[:, :table.shape[1]] = table.cuda()
+    want = binding.lora_paged_attn_fwd(q.cuda(), cache, table.cuda(), offsets.cuda(), lens.cuda(), 70, 130)
+    out = torch.zeros_like(wide)
+    binding.lora_paged_attn_fwd(wide[:, :H * D].unflatten(1, (H, D)), cache, pages[:, :table.shape[1]], offsets.cuda(), lens.cuda(), 70, 130,
+                                out=out[:, H * D // 2:H * D // 2 + H * D].unflatten(1, (H, D)))
+    assert torch.equal(out[:, H * D // 2:H * D // 2 + H * D].unflatten(1, (H, D)), want)
+    assert not out[:, :H * D // 2].any() and not out[:, H * D // 2 + H * D:].any()
+
+
+def test_cache_past_32_bits():
+    """Pages whose bytes start past 2^32."""
+    pages, page, G, D = (1 << 31) // (64 * 2 * 128) + 2, 64, 2, 128
+    cache = binding.KVCache.empty(pages, page, G, D, False)
+    g = gen(3)
+    k, v = normal(g, (100, G, D)), normal(g, (100, G, D))
+    table = torch.tensor([[pages - 1, pages - 2]], dtype=torch.int32)
+    slots = torch.cat([torch.arange(64) + (pages - 1) * 64, torch.arange(36) + (pages - 2) * 64])
+    binding.lora_kv_cache_write(cache, k.cuda(), v.cuda(), slots.cuda())
+    for n in (1, 50):
+        q = normal(g, (n, 4, D))
+        out = binding.lora_paged_attn_fwd(q.cuda(), cache, table.cuda(), torch.tensor([0, n], dtype=torch.int32).cuda(),
+                                          torch.tensor([100], dtype=torch.int32).cuda(), n, 100)
+        ref, bound = attention(q.to(F64), k.to(F64), v.to(F64), n, 100, D ** -0.5, 0)
+        within(out, ref, bound, n)
+
+
+def test_not_finite_query_stays_in_its_row():
+    for n in (2, 60):
+        q, cache, table, offsets, lens, _ = _setup([(n, n + 70)], 4, 2, 64, 16, False, 2)
+        q[1, 2, 5] = NAN
+        out = binding.lora_paged_attn_fwd(q.cuda(), cache, table.cuda(), offsets.cuda(), lens.cuda(), n, n + 70)
+        bad = (~torch.isfinite(out)).any(-1).cpu()
+        want = torch.zeros((n, 4), dtype=torch.bool)
+        want[1, 2] = True
+        assert torch.equal(bad, want)
+
+
+def test_arguments():
+    q, cache, table, offsets, lens, _ = _setup([(2, 30)], 4, 2, 64, 16, False, 1)
+    q, table, offsets, lens = (t.cuda() for t in (q, table, offsets, lens))
+    f = binding.lora_paged_attn_fwd
+    for bad in ((q.float(), cache, table, offsets, lens), (q, cache, table.long(), offsets, lens), (q, cache, table, offsets[:1], lens),
+                (q, cache, table, offsets, lens.long()), (q[..., :32], cache, table, offsets, lens)):
+        with pytest.raises(AssertionError):
+            f(*bad, 2, 30)
+    for kw in (dict(scale=0.0), dict(window=-1)):
+        with pytest.raises(binding.LoraError):
+            f(q, cache, table, offsets, lens, 2, 30, **kw)
+    with pytest.raises(binding.LoraError):
+        f(q[:, :3], cache, table, offsets, lens, 2, 30)
+    assert f(q[:0], cache, table, torch.zeros(2, dtype=torch.int32, device="cuda"), lens, 0, 30).shape == (0, 4, 64)
