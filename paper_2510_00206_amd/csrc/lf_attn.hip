@@ -17,13 +17,14 @@
 //
 // The fp8 form of the cache is widened to bf16 (exact: e4m3 times a power of two) on the way to LDS or into the fragments.
 #include <algorithm>
+#include <type_traits>
 
 #include "lf_gemm_parts.h"
 #include "lf_serve.h"
 
 namespace lf {
 
-constexpr float kNone = -__builtin_inff();
+constexpr float kNone = -1e30f;                  // reference of a row that has seen nothing: finite, so that every p against it is 0 and no case of its own
 
 // What a workgroup works on.
 struct AttnTile {
@@ -52,27 +53,35 @@ __device__ __forceinline__ bool attn_rows(const AttnArgs& p, AttnTile& t) {
 
 template <int BM>
 __device__ __forceinline__ bool attn_tile(const AttnArgs& p, AttnTile& t) {
-    // Key/value heads of a sequence fastest, then sequences: with eight heads the tiles and parts that share keys are on one XCD.  Last tiles
-    // first: they see the most keys.
+    // Key/value heads of a sequence fastest: with eight heads the tiles that share keys are on one XCD.  Then tiles, the last first, since they see the
+    // most keys; parts slowest: the last ones, which hold what is left of a range, run last.  Within an XCD workgroups go to its four
+    // shader engines in turn, full or not: with sequences before tiles, two of them (5003 and 16000 keys, 1021 new tokens) left half
+    // the engines without work for half of the time (515 us instead of 363).
     int id = blockIdx.x;
     t.g = id % p.c.heads;
     id /= p.c.heads;
+    t.tile = p.tiles - 1 - id % p.tiles;
+    id /= p.tiles;
     t.b = id % p.B;
-    id /= p.B;
-    t.split = id % p.splits;
-    t.tile = p.tiles - 1 - id / p.splits;
+    t.split = id / p.B;
     if (!attn_rows<BM>(p, t) || t.split >= t.parts) return false;
     t.k0 = t.key_lo + t.split * p.split_keys;
     t.k1 = t.split + 1 == p.splits ? t.key_hi : min(t.key_hi, t.k0 + p.split_keys);     // (the last takes what there is: lengths past max_kv)
     return true;
 }
 
-// Element offset of the first key of a 16-key block (in one page) of head g, in units of a head's entries; key < kv.
-__device__ __forceinline__ int64_t attn_block(const AttnArgs& p, const AttnTile& t, int key) {
-    int64_t page = p.table[(int64_t)t.b * p.ldt + (key >> p.c.page_shift)];
-    page = page < 0 ? 0 : page >= p.c.pages ? p.c.pages - 1 : page;
-    return ((page * p.c.heads + t.g) << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1));
+// Page of a 16-key block that starts at `key` (below the length, the same for the whole wave), as the table has it: a scalar load, asked for a step
+// before it is needed.  A vector load, with the wait for it before the step's copies could be issued, took a third of the time.
+__device__ __forceinline__ int page_of(const AttnArgs& p, const AttnTile& t, int key) {
+    return ((const __attribute__((address_space(4))) int32_t*)p.table)[(int64_t)t.b * p.ldt + (key >> p.c.page_shift)];
 }
+// Heads (rows of D entries) from the cache's start to the block's first key.
+__device__ __forceinline__ int64_t attn_block(const AttnArgs& p, const AttnTile& t, int page, int key) {
+    const uint32_t at = min((uint32_t)page, (uint32_t)p.c.pages - 1u);          // (below zero: past the end)
+    return (int64_t)((uint64_t)at * (uint32_t)(p.c.heads << p.c.page_shift)) + ((t.g << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1)));
+}
+// Block `b` of the tile at `key`, or the last one that has keys.
+__device__ __forceinline__ int block_key(const AttnTile& t, int key, int b) { return min(key + 16 * b, t.k1 - 1) & ~15; }
 
 __device__ __forceinline__ float scale_of(uint8_t e) { return ldexpf(1.f, (int)e - 127); }
 
@@ -100,47 +109,134 @@ __device__ __forceinline__ bf16x8 v_frag(const char* v, int r0, int block) {
     return join_tr(lds_read_tr(v, off), lds_read_tr(v, off + 16 * 2 * D));      // (16 rows further: the same swizzle)
 }
 
-// Running maximum and sum of the 16 queries of a block; m is the same in the four lanes of a query, l its lane's own part of the sum.
-struct Running { float m, l; };
-
-// Softmax step over KB blocks of 16 keys: s holds scores and then p (both as four keys a block); returns what the sums so far are multiplied by.
+// Largest of a lane's scores, in steps of two: number n of 2 KB (the last with one score).  Written as such: from fmaxf the compiler makes an
+// instruction more for every score, to quiet NaNs.  It does not know the distance that the matrix pipe's results need before these
+// read them: nine wait states stand before the first, or eight other instructions.
 template <int KB>
-__device__ __forceinline__ float softmax_step(f32x4 (&s)[KB], Running& r, float scale) {
-    float top = kNone;
-#pragma unroll
-    for (int b = 0; b < KB; ++b) top = fmaxf(fmaxf(fmaxf(top, s[b][0]), fmaxf(s[b][1], s[b][2])), s[b][3]);
-    top = over_quarters(top, [](float a, float b) { return fmaxf(a, b); });
-    const float m = fmaxf(r.m, top * scale);
-    const float base = m == kNone ? 0.f : m;               // nothing seen yet: every p is 0
-    const float back = __builtin_amdgcn_exp2f(r.m - base);
-    float sum = 0.f;
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], scale, -base));
-            sum += s[b][e];
-        }
-    r.m = m;
-    r.l = r.l * back + sum;
-    return back;
+__device__ __forceinline__ void top_step(float& top, const f32x4 (&s)[KB], int n) {
+    const float x = s[n / 2][n % 2 * 2], y = s[n / 2][n % 2 * 2 + 1];
+    if (n == 0) asm volatile("v_max_f32 %0, %1, %2" : "=v"(top) : "v"(x), "v"(y));
+    else asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(top) : "v"(x), "v"(y));
 }
+// The larger of this lane's and of that 16 (ROW; otherwise 32) lanes away.
+template <bool ROW>
+__device__ __forceinline__ void top_over_lanes(float& top) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, top);
+    const auto both = ROW ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    asm("v_max_f32 %0, %1, %2" : "=v"(top) : "v"((uint32_t)both[0]), "v"((uint32_t)both[1]));
+}
+template <int KB>
+__device__ __forceinline__ float top_of(const f32x4 (&s)[KB]) {
+    float top;
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 8");
+#pragma unroll
+    for (int n = 0; n < 2 * KB; ++n) top_step<KB>(top, s, n);
+    top_over_lanes<true>(top);
+    top_over_lanes<false>(top);
+    return top;
+}
+
+// p = 2^(scale s - m).  m is the reference of the 16 queries of a block, the same in the four lanes of a query.  It follows the largest score only
+// when that is more than 2^8 above it, so that most steps leave the sums as they are (p of up to 2^8 are as exact as those below
+// 1).  Returns whether any has moved; back: what the sums are to be multiplied by.
+// top: over the four lanes of a query.
+template <int NQ>
+__device__ __forceinline__ bool follow(const float (&top)[NQ], float (&m)[NQ], float (&back)[NQ], float scale) {
+    bool rises = false;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) rises |= __builtin_fmaf(top[i], scale, -m[i]) > 8.f;
+    if (!__any(rises)) return false;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const float to = __builtin_fmaf(top[i], scale, -m[i]) > 8.f ? top[i] * scale : m[i];
+        back[i] = to == m[i] ? 1.f : __builtin_amdgcn_exp2f(m[i] - to);
+        m[i] = to;
+    }
+    return true;
+}
+__device__ __forceinline__ float p_of(float s, float scale, float m) { return __builtin_amdgcn_exp2f(__builtin_fmaf(s, scale, -m)); }
+
+// The lane's number, formed where it is asked for: in code that runs rarely, or after a loop, so that nothing derived from it is kept through the loop.
+__device__ __forceinline__ int lane_here() {
+    int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(l));
+    return l;
+}
+
+__device__ __forceinline__ bool sees(int pos, int key, int window) { return key <= pos && (!window || key > pos - window); }
 
 // Hides from query `pos` what it may not see of the keys key0 + 16 b + 4 q + e.
 template <int KB>
 __device__ __forceinline__ void hide(f32x4 (&s)[KB], int key0, int pos, int window) {
-    const int q4 = (threadIdx.x & 63) >> 4 << 2;
+    const int q4 = lane_here() >> 4 << 2;
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int key = key0 + 16 * b + q4 + e;
-            if (key > pos || (window && key <= pos - window)) s[b][e] = kNone;
+            if (!sees(pos, key0 + 16 * b + q4 + e, window)) s[b][e] = -__builtin_inff();
         }
 }
 
-__device__ __forceinline__ bf16x8 p_frag(f32x4 a, f32x4 b) {
-    return __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])});
+// A lane's sum of the p that it holds: of the rounded ones, as the product takes them.
+__device__ __forceinline__ float add_pair(uint32_t p2, float sum) {
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p2), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+}
+
+// O^T += V^T P^T over the 32 keys of a tile of values.  Fragments are read two ahead of their use.
+template <int D, int NQ>
+__device__ __forceinline__ void add_values(f32x4 (&o)[NQ][D / 16], const bf16x8 (&pf)[NQ], const char* v) {
+    constexpr int DB = D / 16;
+    bf16x8 vf[3];
+    vf[0] = v_frag<D>(v, 0, 0);
+    vf[1] = v_frag<D>(v, 0, 1);
+#pragma unroll
+    for (int n = 0; n < DB; ++n) {
+        if (n + 2 < DB) vf[(n + 2) % 3] = v_frag<D>(v, 0, n + 2);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) o[i][n] = LF_MFMA(vf[n % 3], pf[i], o[i][n]);
+    }
+}
+
+// Tiles of which some rows see a part: 0 x infinity or NaN must not reach a row that does not see the key.  What is not finite is cleared on
+// its way into LDS and, if there is any, read again and added key by key to the rows that see the key.
+__device__ __forceinline__ u32x4 not_finite(u32x4 v) {       // 0xFFFF in the halves that are
+    u32x4 m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = v[i] & 0x7FFF7FFFu;
+        m[i] = ((x & 0xFFFFu) >= 0x7F80u ? 0xFFFFu : 0u) | (x >= 0x7F800000u ? 0xFFFF0000u : 0u);
+    }
+    return m;
+}
+template <int D, bool FP8, int NQ, int KB>
+__device__ __forceinline__ void add_not_finite(const AttnArgs& p, const AttnTile& t, f32x4 (&o)[NQ][D / 16], const int (&pos)[NQ], int key0) {
+    const int q = lane_here() >> 4;
+#pragma unroll 1
+    for (int k = 0; k < min(16 * KB, t.k1 - key0); ++k) {
+        const int at16 = (key0 + k) & ~15;
+        const int64_t at = attn_block(p, t, page_of(p, t, at16), at16) + (k & 15);
+        const char* row = (const char*)p.c.v + at * (D * (FP8 ? 1 : 2)) + q * (FP8 ? 4 : 8);
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+            u32x2 x;
+            if constexpr (FP8) {
+                const uint32_t y = *(const uint32_t*)(row + 16 * d);
+                x = __builtin_bit_cast(u32x4, widen8(y, y, scale_of(p.c.v_exp[at]))).xy;
+            } else {
+                x = *(const u32x2*)(row + 32 * d);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t y = e & 1 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16;
+                const bool bad = (y & 0x7F800000u) == 0x7F800000u;
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) o[i][d][e] += bad && sees(pos[i], key0 + k, p.window) ? __builtin_bit_cast(float, y) : 0.f;
+            }
+        }
+    }
 }
 
 // Position of the token of row `row` (of the tile's sequence and head).
@@ -167,6 +263,14 @@ __device__ __forceinline__ void put(const AttnArgs& p, const AttnTile& t, int ro
     v.x = pack_bf16x2(o[0] * inv, o[1] * inv);
     v.y = pack_bf16x2(o[2] * inv, o[3] * inv);
     *(u32x2*)(p.out + (int64_t)(t.first + tok) * p.ldo + (int64_t)head * p.c.D + d) = v;
+}
+
+// The fragments have come in: the waits for them stand here, not where they are used, in the loops, where they would be for whatever the loops have
+// asked for in the meantime.
+template <int N>
+__device__ __forceinline__ void have(bf16x8 (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
 }
 
 // ---- few rows --------------------------------------------------------------------------------------
@@ -204,11 +308,14 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
             qf[i][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(src + (FP8 ? 64 * (kk / 2) + 16 * q + 8 * (kk & 1) : 32 * kk + 8 * q)));
     }
     const int pos_lo = pos_of(p, t, t.row0);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) have(qf[i]);
     f32x4 o[NQ][DB];
-    Running run[NQ];
+    float m[NQ], sum[NQ];
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        run[i] = Running{kNone, 0.f};
+        m[i] = kNone;
+        sum[i] = 0.f;
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[i][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -217,10 +324,15 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
     uint8_t ke[2], ve[C::VL];
     const char *kc = (const char*)p.c.k, *vc = (const char*)p.c.v;
     constexpr int ESZ = FP8 ? 1 : 2, LANES = D * ESZ / 16;          // lanes to a row of values
+    int pages[2];                                           // of the blocks of the tile that is asked for next
     int64_t blk[2];
+    auto look_up = [&](int key) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) pages[b] = page_of(p, t, block_key(t, key, b));
+    };
     auto find = [&](int key) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) blk[b] = attn_block(p, t, min(key + 16 * b, t.k1 - 1) & ~15);
+        for (int b = 0; b < 2; ++b) blk[b] = attn_block(p, t, pages[b], block_key(t, key, b));
     };
     auto load_k = [&]() {
 #pragma unroll
@@ -241,31 +353,53 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
         }
     };
 
+    constexpr int STEP = C::WAVES * C::KEYS;
     int key = t.k0 + C::KEYS * w;
     if (key < t.k1) {
+        look_up(key);
         find(key);
+        look_up(key + STEP);
         load_k();
         load_v();
     }
-    for (; key < t.k1; key += C::WAVES * C::KEYS) {
-        const bool more = key + C::WAVES * C::KEYS < t.k1;
+    for (; key < t.k1; key += STEP) {
+        const bool more = key + STEP < t.k1;
+        const bool whole = key + C::KEYS - 1 <= pos_lo && (!p.window || key > pos_of(p, t, t.row0 + t.rows - 1) - p.window);
+        bool bad = false;                                    // a value that is not finite, where that matters
         // values to LDS; a row past the end holds anything, and 0 x anything need not be 0
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int i = 0; i < C::VL; ++i) {
             const int row = i * (64 / LANES) + l / LANES, ch = l % LANES;
             const bool in = key + row < t.k1;
+            u32x4 lo = vr[i], hi;
             if constexpr (FP8) {
                 const float sc = scale_of(ve[i]);
-                const bf16x8 lo = widen8(vr[i][0], vr[i][1], sc), hi = widen8(vr[i][2], vr[i][3], sc);
-                *(u32x4*)(mine + v_off<D>(row, 2 * ch)) = in ? __builtin_bit_cast(u32x4, lo) : u32x4{0u, 0u, 0u, 0u};
-                *(u32x4*)(mine + v_off<D>(row, 2 * ch + 1)) = in ? __builtin_bit_cast(u32x4, hi) : u32x4{0u, 0u, 0u, 0u};
+                lo = __builtin_bit_cast(u32x4, widen8(vr[i][0], vr[i][1], sc));
+                hi = __builtin_bit_cast(u32x4, widen8(vr[i][2], vr[i][3], sc));
+            }
+            if (!whole) {
+                lo = in ? lo : u32x4{0u, 0u, 0u, 0u};
+                u32x4 m = not_finite(lo);
+                lo &= ~m;
+                if constexpr (FP8) {
+                    hi = in ? hi : u32x4{0u, 0u, 0u, 0u};
+                    const u32x4 mh = not_finite(hi);
+                    hi &= ~mh;
+                    m |= mh;
+                }
+                bad |= (m[0] | m[1] | m[2] | m[3]) != 0;
+            }
+            if constexpr (FP8) {
+                *(u32x4*)(mine + v_off<D>(row, 2 * ch)) = lo;
+                *(u32x4*)(mine + v_off<D>(row, 2 * ch + 1)) = hi;
             } else {
-                *(u32x4*)(mine + v_off<D>(row, ch)) = in ? vr[i] : u32x4{0u, 0u, 0u, 0u};
+                *(u32x4*)(mine + v_off<D>(row, ch)) = lo;
             }
         }
         if (more) {
-            find(key + C::WAVES * C::KEYS);
+            find(key + STEP);
+            look_up(key + 2 * STEP);
             load_v();
         }
         f32x4 s[NQ][2];
@@ -286,50 +420,59 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
                 for (int i = 0; i < NQ; ++i) s[i][b] = LF_MFMA(kf, qf[i][kk], s[i][b]);
             }
         if (more) load_k();
-        const bool whole = key + C::KEYS - 1 <= pos_lo && (!p.window || key > pos_of(p, t, t.row0 + t.rows - 1) - p.window);
-        bf16x8 pf[NQ];
+        float top[NQ], back[NQ];
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             if (!whole) hide(s[i], key, pos[i], p.window);
-            const float back = softmax_step(s[i], run[i], p.scale);
-            pf[i] = p_frag(s[i][0], s[i][1]);
-            if (__any(back != 1.f))
+            top[i] = top_of<2>(s[i]);
+        }
+        if (follow<NQ>(top, m, back, p.scale))
 #pragma unroll
-                for (int d = 0; d < DB; ++d) o[i][d] *= back;
+            for (int i = 0; i < NQ; ++i) {
+                sum[i] *= back[i];
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[i][d] *= back[i];
+            }
+        bf16x8 pf[NQ];
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            u32x4 pw;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4& x = s[i][j / 2];
+                pw[j] = pack_bf16x2(p_of(x[j % 2 * 2], p.scale, m[i]), p_of(x[j % 2 * 2 + 1], p.scale, m[i]));
+                sum[i] = add_pair(pw[j], sum[i]);
+            }
+            pf[i] = __builtin_bit_cast(bf16x8, pw);
         }
         asm volatile("" ::: "memory");
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            const bf16x8 vf = v_frag<D>(mine, 0, d);
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) o[i][d] = LF_MFMA(vf, pf[i], o[i][d]);
-        }
+        add_values<D, NQ>(o, pf, mine);
+        if (__any(bad)) add_not_finite<D, FP8, NQ, 2>(p, t, o, pos, key);
     }
 
     // the four waves' sums, brought to one reference
     float* ml = (float*)(smem + C::WAVES * C::WAVE_LDS);              // [row][wave] of m, then of l
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        run[i].l = over_quarters(run[i].l, [](float a, float b) { return a + b; });
+        sum[i] = over_quarters(sum[i], [](float a, float b) { return a + b; });
         if (q == 0) {
-            ml[(16 * i + c) * C::WAVES + w] = run[i].m;
-            ml[(NQ * 16 + 16 * i + c) * C::WAVES + w] = run[i].l;
+            ml[(16 * i + c) * C::WAVES + w] = m[i];
+            ml[(NQ * 16 + 16 * i + c) * C::WAVES + w] = sum[i];
         }
     }
     __syncthreads();
-    const auto joined = [&](int row, float& m, float& sum) {
+    const auto joined = [&](int row, float& top, float& l) {
         const f32x4 a = *(const f32x4*)(ml + row * C::WAVES), b = *(const f32x4*)(ml + (NQ * 16 + row) * C::WAVES);
-        m = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
-        const float base = m == kNone ? 0.f : m;
-        sum = 0.f;
+        top = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+        l = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += b[i] * __builtin_amdgcn_exp2f(a[i] - base);
+        for (int i = 0; i < 4; ++i) l += b[i] * __builtin_amdgcn_exp2f(a[i] - top);
     };
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        float m, sum;
-        joined(16 * i + c, m, sum);
-        const float f = __builtin_amdgcn_exp2f(run[i].m - (m == kNone ? 0.f : m));
+        float top, l;
+        joined(16 * i + c, top, l);
+        const float f = __builtin_amdgcn_exp2f(m[i] - top);
 #pragma unroll
         for (int d = 0; d < DB; ++d) *(f32x4*)(mine + ((16 * i + c) * D + (((4 * d + q) ^ c) << 2)) * 4) = o[i][d] * f;
     }
@@ -339,24 +482,59 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
         f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < C::WAVES; ++k) v += *(const f32x4*)(smem + k * C::WAVE_LDS + (row * D + ((ch ^ (row & 15)) << 2)) * 4);
-        float m, sum;
-        joined(row, m, sum);
-        put(p, t, t.row0 + row, 4 * ch, v, m, sum);
+        float top, l;
+        joined(row, top, l);
+        put(p, t, t.row0 + row, 4 * ch, v, top, l);
     }
 }
 
+// f(0), f(1), .., f(N - 1), each with its number as a constant.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void each(F&& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
+// How many of `items`, spread over `slots`, come before slot n.
+constexpr int slots_before(int n, int items, int slots) { return n <= 0 ? 0 : n >= slots ? items : (n * items + slots - 1) / slots; }
+
 // ---- many rows --------------------------------------------------------------------------------------
-template <int D>
+template <int D, bool FP8>
 struct Many {
     static constexpr int KEYS = 64, ROWS = 128, NQ = 2;
-    static constexpr int TILE = KEYS * D * 2, STAGE = 2 * TILE, LDS = 2 * STAGE;
+    static constexpr int TILE = KEYS * D * 2, FLAGS = 4 * TILE, RAW = FLAGS + 16;      // two tiles of keys, two of values; flags; fp8 a tile as it is held
+    static constexpr int LDS = RAW + (FP8 ? KEYS * D : 0);
 };
+
+// Copy I of a block of 16 keys (or values) into LDS, 1 KB: the instruction's offset, the same for memory and LDS, counts from the middle.  The first
+// sets M0 for the others.
+template <int D, bool KEYS, int I>
+__device__ __forceinline__ void copy_one(const char* from, uint32_t lane, uint32_t m0) {
+    constexpr int NP = D / 32, RPC = 512 / D;
+    const uint32_t swz = (KEYS ? k_off<D>(RPC * I, 0) : v_off<D>(RPC * I, 0)) & (2 * D - 1);
+    copy16_to_lds<pass_imm(NP, I), I == 0>(from + NP / 2 * 1024, lane ^ swz, m0);
+}
+template <int D, bool KEYS, int I = 0>
+__device__ __forceinline__ void copy_block(const char* from, uint32_t lane, uint32_t m0) {
+    if constexpr (I < D / 32) {
+        copy_one<D, KEYS, I>(from, lane, m0);
+        copy_block<D, KEYS, I + 1>(from, lane, m0);
+    }
+}
+
+template <int NR, int I = 0>
+__device__ __forceinline__ void copy_raw(const char* from, uint32_t lane, uint32_t m0) {
+    if constexpr (I < NR) {
+        copy16_to_lds<I * 1024, I == 0>(from, lane, m0);
+        copy_raw<NR, I + 1>(from, lane, m0);
+    }
+}
 
 template <int D, bool FP8>
 __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
-    using C = Many<D>;
+    using C = Many<D, FP8>;
     constexpr int NQ = C::NQ, KK = D / 32, DB = D / 16, KB = C::KEYS / 16;
-    constexpr int ESZ = FP8 ? 1 : 2, LANES = D * ESZ / 16, RPP = 256 / LANES, L = C::KEYS / RPP;   // rows a pass of the workgroup, passes
     extern __shared__ __attribute__((aligned(16))) char smem[];
     AttnTile t;
     if (!attn_tile<C::ROWS>(p, t)) return;
@@ -372,115 +550,289 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) qf[i][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(src + 32 * kk + 8 * q));
     }
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) have(qf[i]);
     const int pos_lo = pos_of(p, t, t.row0 + min(32 * w, t.rows - 1)), pos_hi = pos_of(p, t, t.row0 + min(32 * w + 31, t.rows - 1));
     f32x4 o[NQ][DB];
-    Running run[NQ];
+    float m[NQ], sum[NQ];
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        run[i] = Running{kNone, 0.f};
+        m[i] = kNone;
+        sum[i] = 0.f;
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[i][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // a thread brings 16 bytes of a row of keys and one of values in each pass
-    u32x4 kr[L], vr[L];
-    uint8_t ke[L], ve[L];
-    const int row_in = threadIdx.x / LANES, ch = threadIdx.x % LANES;
-    auto load = [&](int key) {
+    // Straight into LDS, wave w the 16 keys of block w, which lie side by side in their page; a lane's source chosen so that what it writes lies
+    // swizzled.  fp8: as it is, into a place of the wave's own, from where the wave widens it into the tile.
+    constexpr int RPC = 512 / D;                             // bf16: rows of a 1 KB copy
+    const uint32_t lds = lds_addr_of(smem);
+    // source of a lane in copy 0; in copy i, 1 KB further, only the swizzle differs, by a constant: k_off, v_off of row RPC * i
+    auto lane_source = [&](bool keys) {
+        const int le = lane_here(), row = le / (D / 8);
+        return (uint32_t)((row * 2 * D + le % (D / 8) * 16) ^ ((keys ? k_off<D>(row, 0) : v_off<D>(row, 0)) & (2 * D - 1)));
+    };
+    constexpr int NR = FP8 ? D / 64 : 1, RPR = 1024 / D;     // fp8: copies of a block, rows of one
+    uint8_t ex[NR];                                         // ... and of this lane's row of each the exponent
+    // first head entry of the wave's block in the tiles whose values (at_v) and keys (at_k) are asked for next, and in the one between; page of the
+    // one after
+    int64_t at_v, at_n, at_k;
+    int page_after;
+    auto page_at = [&](int key) { return page_of(p, t, block_key(t, key, w)); };
+    auto block_at = [&](int page, int key) { return attn_block(p, t, page, block_key(t, key, w)); };
+    auto source = [&](bool keys, int64_t at) { return (const char*)(keys ? p.c.k : p.c.v) + at * (FP8 ? D : 2 * D); };
+    // keys (values) into half `stage` of their part of LDS
+    auto bring = [&](bool keys, int64_t at, int stage) {
+        const char* from = source(keys, at);
+        if constexpr (FP8) {
+            copy_raw<NR>(from, lane_here() * 16, __builtin_amdgcn_readfirstlane(lds + C::RAW + w * 16 * D));
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-            const int row = i * RPP + row_in;
-            const int64_t at = attn_block(p, t, min(key + (row & ~15), t.k1 - 1) & ~15) + (row & 15);
-            kr[i] = *(const u32x4*)((const char*)p.c.k + at * (D * ESZ) + ch * 16);
-            vr[i] = *(const u32x4*)((const char*)p.c.v + at * (D * ESZ) + ch * 16);
-            if constexpr (FP8) {
-                ke[i] = p.c.k_exp[at];
-                ve[i] = p.c.v_exp[at];
-            }
+            for (int i = 0; i < NR; ++i) ex[i] = (keys ? p.c.k_exp : p.c.v_exp)[at + i * RPR + lane_here() / (D / 16)];
+        } else {
+            const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds + (keys ? 0 : 2 * C::TILE) + stage * C::TILE + w * 32 * D + D / 64 * 1024);
+            if (keys) copy_block<D, true>(from, lane_source(true), m0);
+            else copy_block<D, false>(from, lane_source(false), m0);
         }
     };
-    auto store = [&](int key, char* st) {
+    // fp8: row and first chunk in the tile of 16 bytes of copy i, and what they are widened to
+    struct Wide { int row, chunk; u32x4 lo, hi; };
+    auto widened = [&](int i) {
+        const int le = lane_here();
+        const u32x4 raw = *(const u32x4*)(smem + C::RAW + w * 16 * D + i * 1024 + le * 16);
+        const float sc = scale_of(ex[i]);
+        return Wide{16 * w + i * RPR + le / (D / 16), le % (D / 16) * 2, __builtin_bit_cast(u32x4, widen8(raw[0], raw[1], sc)),
+                    __builtin_bit_cast(u32x4, widen8(raw[2], raw[3], sc))};
+    };
+    auto brought_k = [&](int stage) {
+        wait_slab_loads();
+        if constexpr (FP8)
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-            const int row = i * RPP + row_in;
-            const u32x4 zero{0u, 0u, 0u, 0u};
-            const bool in = key + row < t.k1;              // a row past the end holds anything, and 0 x anything need not be 0
-            if constexpr (FP8) {
-                const float sk = scale_of(ke[i]), sv = scale_of(ve[i]);
-                *(u32x4*)(st + k_off<D>(row, 2 * ch)) = __builtin_bit_cast(u32x4, widen8(kr[i][0], kr[i][1], sk));
-                *(u32x4*)(st + k_off<D>(row, 2 * ch + 1)) = __builtin_bit_cast(u32x4, widen8(kr[i][2], kr[i][3], sk));
-                const u32x4 lo = __builtin_bit_cast(u32x4, widen8(vr[i][0], vr[i][1], sv)), hi = __builtin_bit_cast(u32x4, widen8(vr[i][2], vr[i][3], sv));
-                *(u32x4*)(st + C::TILE + v_off<D>(row, 2 * ch)) = in ? lo : zero;
-                *(u32x4*)(st + C::TILE + v_off<D>(row, 2 * ch + 1)) = in ? hi : zero;
-            } else {
-                *(u32x4*)(st + k_off<D>(row, ch)) = kr[i];
-                *(u32x4*)(st + C::TILE + v_off<D>(row, ch)) = in ? vr[i] : zero;
+            for (int i = 0; i < NR; ++i) {
+                const Wide x = widened(i);
+                *(u32x4*)(smem + stage * C::TILE + k_off<D>(x.row, x.chunk)) = x.lo;
+                *(u32x4*)(smem + stage * C::TILE + k_off<D>(x.row, x.chunk + 1)) = x.hi;
+            }
+    };
+    // flag of a stage: the number of its tile if a value in it is not finite, where that matters (a tile that not all rows see in whole)
+    const int first_pos = pos_of(p, t, t.row0), last_pos = pos_of(p, t, t.row0 + t.rows - 1);
+    auto all_whole = [&](int key) { return key + C::KEYS - 1 <= first_pos && (!p.window || key > last_pos - p.window); };
+    int* flags = (int*)(smem + C::FLAGS);
+    auto brought_v = [&](int key, int stage) {
+        char* st = smem + 2 * C::TILE + stage * C::TILE;
+        const bool guard = !all_whole(key);
+        bool bad = false;
+        // a row past the end holds anything, and 0 x anything need not be 0
+        auto guarded = [&](u32x4 x, int row) {
+            if (key + row >= t.k1) x = u32x4{0u, 0u, 0u, 0u};
+            const u32x4 m = not_finite(x);
+            bad |= (m[0] | m[1] | m[2] | m[3]) != 0;
+            return x & ~m;
+        };
+        wait_slab_loads();
+        if constexpr (FP8) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                Wide x = widened(i);
+                if (guard) {
+                    x.lo = guarded(x.lo, x.row);
+                    x.hi = guarded(x.hi, x.row);
+                }
+                *(u32x4*)(st + v_off<D>(x.row, x.chunk)) = x.lo;
+                *(u32x4*)(st + v_off<D>(x.row, x.chunk + 1)) = x.hi;
+            }
+        } else if (guard) {
+            for (int i = lane_here(); i < 2 * D; i += 64) {  // the wave's own 16 rows, chunk by chunk
+                u32x4* at = (u32x4*)(st + w * 32 * D + i * 16);
+                *at = guarded(*at, 16 * w + i / (D / 8));
             }
         }
+        if (__any(bad) && lane_here() == 0) flags[stage] = key;
     };
 
-    int stage = 0;
+    // Step n forms the scores of tile n + 1 and adds the values of tile n - 1, while between these matrix instructions the exponentials of tile n
+    // and then the maxima of tile n + 1 run: the vector unit can work beside the matrix pipe only between the matrix instructions
+    // of the same wave (two to three instructions to each; those of another wave of the SIMD wait), so every one gets its share.
+    constexpr int AHEAD = 2, FK = KB * KK, FV = KB / 2 * DB;       // fragments on their way from LDS; fragments of a tile
+    constexpr int NS = FK * NQ, NV = FV * NQ;                      // matrix instructions of the scores and of the values
+    constexpr int EXPS = 4 * KB * NQ, EXP_SLOTS = NS, TOPS = 2 * KB * NQ, TOP_FROM = NS + NV / 3, TOP_SLOTS = NV / 3;
+    constexpr int LANES_FROM = TOP_FROM + TOP_SLOTS, LANES_SLOTS = NS + NV - LANES_FROM;
+    bf16x8 fr[AHEAD + 1];
+    const char *kst, *vst;
+    auto read_k = [&](int f) {
+        if (f < FK) fr[f % (AHEAD + 1)] = __builtin_bit_cast(bf16x8, *(const u32x4*)(kst + k_off<D>(16 * (f / KK) + c, 4 * (f % KK) + q)));
+    };
+    auto read_v = [&](int f) {
+        if (f < FV) fr[(FK + f) % (AHEAD + 1)] = v_frag<D>(vst, 32 * (f / DB), f % DB);
+    };
+    struct Weights { uint32_t w[NQ][KB / 2][4]; };          // P of a tile, two to a word
+    f32x4 sa[NQ][KB], sb[NQ][KB];                           // scores and weights of this tile and its neighbour, in turn
+    Weights wa, wb;
+    float top[NQ], add[NQ];                                 // of the next tile's scores; sums of this tile's weights
+    auto weigh = [&](f32x4 (&s)[NQ][KB], Weights& pw, int n) {
+        const int i = n / (4 * KB), b = n / 4 % KB, e = n & 3;
+        f32x4& x = s[i][b];
+        x[e] = p_of(x[e], p.scale, m[i]);
+        if (e & 1) {
+            uint32_t& two = pw.w[i][b / 2][2 * (b & 1) + e / 2];
+            two = pack_bf16x2(x[e - 1], x[e]);
+            add[i] = add_pair(two, add[i]);
+        }
+    };
+    auto pfrag = [&](const Weights& pw, int i, int h) { return __builtin_bit_cast(bf16x8, u32x4{pw.w[i][h][0], pw.w[i][h][1], pw.w[i][h][2], pw.w[i][h][3]}); };
+    auto score = [&](f32x4 (&next)[NQ][KB], int n) {        // matrix instruction n of the scores
+        const int f = n / NQ, b = f / KK, i = n % NQ;
+        if (f % KK == 0) next[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        next[i][b] = LF_MFMA(fr[f % (AHEAD + 1)], qf[i][f % KK], next[i][b]);
+    };
+    auto value = [&](const Weights& pw, int n) {            // ... of the values
+        const int f = n / NQ, i = n % NQ;
+        if (i == 0) read_v(f + AHEAD);
+        o[i][f % DB] = LF_MFMA(fr[(FK + f) % (AHEAD + 1)], pfrag(pw, i, f / DB), o[i][f % DB]);
+    };
+
+    if (threadIdx.x < 2) flags[threadIdx.x] = -1;
+    // what step 0 takes for the values of a tile before it
+    for (int i = threadIdx.x; i < C::TILE / 16; i += 256) *(u32x4*)(smem + 3 * C::TILE + i * 16) = u32x4{0u, 0u, 0u, 0u};
     if (t.k0 < t.k1) {
-        load(t.k0);
-        store(t.k0, smem);
+        at_v = block_at(page_at(t.k0), t.k0);
+        at_n = block_at(page_at(t.k0 + C::KEYS), t.k0 + C::KEYS);
+        at_k = block_at(page_at(t.k0 + 2 * C::KEYS), t.k0 + 2 * C::KEYS);
+        page_after = page_at(t.k0 + 3 * C::KEYS);
+        bring(true, at_v, 0);
+        brought_k(0);
+        bring(true, at_n, 1);
+        brought_k(1);
     }
     __syncthreads();
-    for (int key = t.k0; key < t.k1; key += C::KEYS) {
-        const bool more = key + C::KEYS < t.k1;
-        if (more) load(key + C::KEYS);
-        const char* st = smem + stage * C::STAGE;
-        // (a wave whose rows see nothing of the tile leaves it out)
-        if (key <= pos_hi && (!p.window || key + C::KEYS - 1 > pos_lo - p.window)) {
-            f32x4 s[NQ][KB];
+    // the first tile's scores by themselves
+    kst = smem;
+    if (t.k0 < t.k1) {
 #pragma unroll
-            for (int b = 0; b < KB; ++b) {
+        for (int f = 0; f < AHEAD; ++f) read_k(f);
 #pragma unroll
-                for (int i = 0; i < NQ; ++i) s[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NS; ++n) {
+            if (n % NQ == 0) read_k(n / NQ + AHEAD);
+            score(sa, n);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) {
-                    const bf16x8 kf = __builtin_bit_cast(bf16x8, *(const u32x4*)(st + k_off<D>(16 * b + c, 4 * kk + q)));
+        for (int i = 0; i < NQ; ++i) top[i] = top_of<KB>(sa[i]);
 #pragma unroll
-                    for (int i = 0; i < NQ; ++i) s[i][b] = LF_MFMA(kf, qf[i][kk], s[i][b]);
-                }
-            }
-            const bool whole = key + C::KEYS - 1 <= pos_lo && (!p.window || key > pos_hi - p.window);
-            bf16x8 pf[NQ][KB / 2];
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+            for (int h = 0; h < KB / 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) wb.w[i][h][j] = 0u;
+    }
+    __syncthreads();
+    auto step = [&](f32x4 (&s)[NQ][KB], f32x4 (&next)[NQ][KB], Weights& pw, const Weights& before, int key, int stage) {
+        // keys of tile n + 2 to where those of tile n were, values of tile n to where those of tile n - 2 were; bf16: copy by copy between the
+        // matrix instructions, since a copy holds the wave up until the memory pipeline takes it
+        constexpr int NP = D / 32, EVERY = 2;
+        const char *from_k = nullptr, *from_v = nullptr;
+        uint32_t lane_k = 0, lane_v = 0, m0_k = 0, m0_v = 0;
+        const int64_t at_v_now = at_v;
+        if constexpr (FP8) {
+            bring(true, at_k, stage);
+        } else {
+            from_k = source(true, at_k);
+            from_v = source(false, at_v);
+            m0_k = __builtin_amdgcn_readfirstlane(lds + stage * C::TILE + w * 32 * D + D / 64 * 1024);
+            m0_v = m0_k + 2 * C::TILE;
+            lane_k = lane_source(true);
+            lane_v = lane_source(false);
+        }
+        kst = smem + (stage ^ 1) * C::TILE;
+        vst = smem + 2 * C::TILE + (stage ^ 1) * C::TILE;
+#pragma unroll
+        for (int f = 0; f < AHEAD; ++f) read_k(f);
+        const bool whole = key + C::KEYS - 1 <= pos_lo && (!p.window || key > pos_hi - p.window);
+        float back[NQ];
+        if (!whole)
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
-                if (!whole) hide(s[i], key, pos[i], p.window);
-                const float back = softmax_step(s[i], run[i], p.scale);
-#pragma unroll
-                for (int b = 0; b < KB / 2; ++b) pf[i][b] = p_frag(s[i][2 * b], s[i][2 * b + 1]);
-                if (__any(back != 1.f))
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) o[i][d] *= back;
+                hide(s[i], key, pos[i], p.window);
+                top[i] = top_of<KB>(s[i]);
             }
+        const bool moved = follow<NQ>(top, m, back, p.scale);
 #pragma unroll
-            for (int b = 0; b < KB / 2; ++b)
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const bf16x8 vf = v_frag<D>(st + C::TILE, 32 * b, d);
-#pragma unroll
-                    for (int i = 0; i < NQ; ++i) o[i][d] = LF_MFMA(vf, pf[i][b], o[i][d]);
+        for (int i = 0; i < NQ; ++i) add[i] = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+        each<NS + NV>([&](auto slot) {
+            constexpr int n = slot();
+            if constexpr (n < NS) {
+                if constexpr (n % NQ == 0) {
+                    read_k(n / NQ + AHEAD);
+                    if constexpr (n / NQ + AHEAD >= FK) read_v(n / NQ + AHEAD - FK);
                 }
+                score(next, n);
+            } else {
+                value(before, n - NS);
+            }
+            constexpr int e0 = slots_before(n, EXPS, EXP_SLOTS), e1 = slots_before(n + 1, EXPS, EXP_SLOTS);
+            each<e1 - e0>([&](auto k) { weigh(s, pw, e0 + k()); });
+            constexpr int t0 = slots_before(n - TOP_FROM, TOPS, TOP_SLOTS), t1 = slots_before(n + 1 - TOP_FROM, TOPS, TOP_SLOTS);
+            each<t1 - t0>([&](auto k) { top_step<KB>(top[(t0 + k()) / (2 * KB)], next[(t0 + k()) / (2 * KB)], (t0 + k()) % (2 * KB)); });
+            constexpr int l0 = slots_before(n - LANES_FROM, 2 * NQ, LANES_SLOTS), l1 = slots_before(n + 1 - LANES_FROM, 2 * NQ, LANES_SLOTS);
+            each<l1 - l0>([&](auto k) { top_over_lanes<(l0 + k()) / NQ == 0>(top[(l0 + k()) % NQ]); });
+            if constexpr (n == NS + 2) {                    // where the next tiles lie
+                at_v = at_n;
+                at_n = at_k;
+                at_k = block_at(page_after, key + 3 * C::KEYS);
+                page_after = page_at(key + 4 * C::KEYS);
+            }
+            if constexpr (!FP8 && n % EVERY == EVERY - 1 && n / EVERY < 2 * NP) {
+                constexpr int j = n / EVERY;
+                if constexpr (j < NP) copy_one<D, true, j>(from_k, lane_k, m0_k);
+                else copy_one<D, false, j - NP>(from_v, lane_v, m0_v);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (FP8 && n == NS - 1) {             // (one place for what is to be widened)
+                brought_k(stage);
+                bring(false, at_v_now, stage);
+            }
+        });
+        if (key > t.k0 && !all_whole(key - C::KEYS) && flags[stage ^ 1] == key - C::KEYS)
+            add_not_finite<D, FP8, NQ, KB>(p, t, o, pos, key - C::KEYS);
+        if (moved) {
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                sum[i] *= back[i];
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[i][d] *= back[i];
+            }
         }
-        // the other stage was last read before the barrier that began this step
-        stage ^= 1;
-        if (more) store(key + C::KEYS, smem + stage * C::STAGE);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) sum[i] += add[i];
+        brought_v(key, stage);
         __syncthreads();
+    };
+    // (an even number of tiles: only the last part of a range can have an odd one, and no row sees keys past its end)
+    int key = t.k0;
+    for (; key < t.k1; key += 2 * C::KEYS) {
+        step(sa, sb, wa, wb, key, 0);
+        step(sb, sa, wb, wa, key + C::KEYS, 1);
+    }
+    if (t.k0 < t.k1) {
+        vst = smem + 3 * C::TILE;
+#pragma unroll
+        for (int f = 0; f < AHEAD; ++f) read_v(f);
+#pragma unroll
+        for (int n = 0; n < NV; ++n) value(wb, n);
+        if (flags[1] == key - C::KEYS) add_not_finite<D, FP8, NQ, KB>(p, t, o, pos, key - C::KEYS);
     }
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        const float sum = over_quarters(run[i].l, [](float a, float b) { return a + b; });
-        const int row = 32 * w + 16 * i + c;
+        const float total = over_quarters(sum[i], [](float a, float b) { return a + b; });
+        const int le = lane_here(), row = 32 * w + 16 * i + (le & 15);
         if (row < t.rows)
 #pragma unroll
-            for (int d = 0; d < DB; ++d) put(p, t, t.row0 + row, 16 * d + 4 * q, o[i][d], run[i].m, sum);
+            for (int d = 0; d < DB; ++d) put(p, t, t.row0 + row, 16 * d + 4 * (le >> 4), o[i][d], m[i], total);
     }
 }
 
 // ---- the parts' results, joined ---------------------------------------------------------------------
-// A wave for a row, D / 64 entries to a lane.
+// A wave for a row, D / 64 entries to a lane; lane i holds the maximum and sum of parts i, i + 64, .., and the rows of eight parts are under way together.
 template <int D, int BM>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs p) {
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -496,20 +848,35 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs p) {
     const int tok = row / p.group, head = t.g * p.group + row - tok * p.group;
     const int64_t at = (int64_t)(t.first + tok) * p.H + head, plane = (int64_t)p.T * p.H;
     float m = kNone;
-    for (int i = 0; i < t.parts; ++i) m = fmaxf(m, p.part_ml[2 * (i * plane + at)]);
-    const float base = m == kNone ? 0.f : m;
-    constexpr int E = D / 64;
-    float sum = 0.f, o[E] = {};
-    for (int i = 0; i < t.parts; ++i) {
-        const float f = __builtin_amdgcn_exp2f(p.part_ml[2 * (i * plane + at)] - base);
-        sum += f * p.part_ml[2 * (i * plane + at) + 1];
+    for (int i = l; i < t.parts; i += 64) m = fmaxf(m, p.part_ml[2 * (i * plane + at)]);
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += f * p.part_o[(i * plane + at) * D + E * l + e];
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    constexpr int E = D / 64, U = 8;
+    typedef __attribute__((ext_vector_type(E))) float row_t;
+    float sum = 0.f;
+    row_t o = {};
+    for (int i0 = 0; i0 < t.parts; i0 += 64) {
+        float f = 0.f;                                      // of part i0 + l
+        if (i0 + l < t.parts) {
+            const float* ml = p.part_ml + 2 * ((i0 + l) * plane + at);
+            f = __builtin_amdgcn_exp2f(ml[0] - m);
+            sum += f * ml[1];
+        }
+        for (int i = i0; i < min(i0 + 64, t.parts); i += U) {
+            row_t v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = *(const row_t*)(p.part_o + (min(i + u, t.parts - 1) * plane + at) * D + E * l);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u < t.parts) o += v[u] * __shfl(f, (i + u) & 63);
+        }
     }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     lora_bf16* out = p.out + (int64_t)(t.first + tok) * p.ldo + (int64_t)head * D + E * l;
     if constexpr (E == 1) out[0] = (lora_bf16)(pack_bf16x2(o[0] * inv, 0.f) & 0xFFFFu);
-    else *(uint32_t*)out = pack_bf16x2(o[0] * inv, o[1] * inv);
+    else *(uint32_t*)out = pack_bf16x2(o[0] * inv, o[E - 1] * inv);
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
@@ -521,9 +888,16 @@ AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, 
     // the most keys that a tile sees
     int64_t keys = max_kv;
     if (window) keys = std::min<int64_t>(keys, (int64_t)window + (pl.rows + group - 1) / group + 16);
-    // parts of 256 keys and more, until there are four (few rows) or two workgroups to a compute unit
-    const int64_t want = (pl.rows == 128 ? 2 : 4) * kComputeUnits, have = tiles * B * G;
-    int64_t parts = std::max<int64_t>(1, std::min(want / std::max<int64_t>(have, 1), (keys + 255) / 256));
+    // Parts: with few rows, of 512 keys and more, until there are four workgroups to a compute unit; with many, whose parts' results cost 1 KB a
+    // row (D = 128) to write and read again, of 256 and more until there are two, and of 4096 and more until there are eight:
+    // sequences differ in length, and only the device knows how.  us, this rule / others: few rows, 32 sequences of 200 - 4000 keys 32.1 / 33.9
+    // (256, 8 to a compute unit), 64 of 100 - 500 12.4 / 21.5, four of 33000 - 131072 260 / 268; many rows, one sequence of 8192,
+    // 1024 new 154 / 173 (1024, 8), eight of 1000 - 2048, 512 new 141 / 207 (1024, 8).
+    const int64_t have = std::max<int64_t>(tiles * B * G, 1), fill8 = 8 * kComputeUnits / have;
+    const auto in_parts = [&](int64_t least) { return (keys + least - 1) / least; };
+    int64_t parts = pl.rows == 128 ? std::max(std::min<int64_t>(2 * kComputeUnits / have, in_parts(256)), std::min(fill8, in_parts(4096)))
+                                   : std::min<int64_t>(4 * kComputeUnits / have, in_parts(512));
+    parts = std::max<int64_t>(1, parts);
     const int64_t step = 128;
     pl.split_keys = (int)(((keys + parts - 1) / parts + step - 1) / step * step);
     if (pl.split_keys < step) pl.split_keys = step;
@@ -532,21 +906,23 @@ AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, 
     return pl;
 }
 
-template <class K>
-static hipError_t launch_lds(K kernel, int lds, unsigned blocks, const AttnArgs& a, hipStream_t st) {
-    if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+template <auto KERNEL>
+static hipError_t launch_lds(int lds, unsigned blocks, const AttnArgs& a, hipStream_t st) {
+    static bool attr_set = false;                  // one flag per kernel
+    if (!attr_set) {
+        const hipError_t e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
+        attr_set = true;
     }
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), lds, st, a);
+    hipLaunchKernelGGL(KERNEL, dim3(blocks), dim3(256), lds, st, a);
     return hipGetLastError();
 }
 
 template <int D, bool FP8>
 static hipError_t launch_attn_t(const AttnArgs& a, int rows, unsigned blocks, hipStream_t st) {
-    if (rows == 16) return launch_lds(attn_few_kernel<D, FP8, 1>, Few<D, FP8, 1>::LDS, blocks, a, st);
-    if (rows == 32) return launch_lds(attn_few_kernel<D, FP8, 2>, Few<D, FP8, 2>::LDS, blocks, a, st);
-    return launch_lds(attn_many_kernel<D, FP8>, Many<D>::LDS, blocks, a, st);
+    if (rows == 16) return launch_lds<attn_few_kernel<D, FP8, 1>>(Few<D, FP8, 1>::LDS, blocks, a, st);
+    if (rows == 32) return launch_lds<attn_few_kernel<D, FP8, 2>>(Few<D, FP8, 2>::LDS, blocks, a, st);
+    return launch_lds<attn_many_kernel<D, FP8>>(Many<D, FP8>::LDS, blocks, a, st);
 }
 
 template <int D>

@@ -293,57 +293,94 @@ __device__ __forceinline__ void ring_stage(f32x4 (&acc)[C::MI][C::NI], const Rin
     }
 }
 
-// LoRA term of rows with an adapter each, on the accumulators of the wave's MI x NI blocks: one matrix step (two at rank 64) for every
-// adapter among its rows, with the other rows' S left out, so that no value of one adapter meets a row of another, not even multiplied
-// by zero.  S and B come straight from memory in the fragments' layout: an adapter's few rows are read once, and by this wave alone.
+// LoRA term of rows with an adapter each, on the accumulators of the wave's MI x NI blocks: a matrix step for every adapter among its rows
+// (two at rank 64; at rank 16 two adapters share one, each on half of the contraction), with the other rows' S left out, so that no value
+// of one adapter meets a row of another, not even multiplied by zero.  S and B come straight from memory in the fragments' layout:
+// an adapter's few rows are read once, and by this wave alone.  The operands of BATCH steps are under way together, or each
+// step would wait for memory by itself.
 template <class C>
 __device__ __forceinline__ void request_term(const RingRequestArgs& p, f32x4 (&acc)[C::MI][C::NI], const RowTile& rt, int c0, int wm, int wn) {
-    const int l = threadIdx.x & 63;
+    // what the registers hold beside the accumulators and some forty others, with two workgroups on a compute unit where the rings allow two
+    constexpr int WAVES = (C::NW + C::CW) * (2 * C::LDS <= 160 * 1024 ? 2 : 1), HOLD = 512 / ((WAVES + 3) / 4) / 8 * 8;
+    constexpr int FIT = (HOLD - C::MI * C::NI * 4 - 45) / ((C::MI + C::NI) * 4), BATCH = FIT < 1 ? 1 : FIT > 8 ? 8 : FIT;
+    const int l = threadIdx.x & 63, q = l >> 4;
     int id[C::MI];
-    uint32_t todo[C::MI], any = 0;                           // rows (bits) of a block whose adapter is still to come
+    uint32_t todo[C::MI];                                    // rows (bits) of a block whose adapter is still to come
+    bool any = false;
 #pragma unroll
     for (int mi = 0; mi < C::MI; ++mi) {
         const int row = (wm * C::MI + mi) * 16 + (l & 15);
         id[mi] = p.ids[rt.row_start + min(row, rt.rows - 1)];
         if (row >= rt.rows || id[mi] >= p.P) id[mi] = -1;
         todo[mi] = (uint32_t)__ballot(id[mi] >= 0) & 0xFFFFu;
-        any |= todo[mi];
+        any |= todo[mi] != 0;
     }
-    const lora_bf16* brow[C::NI];
+    // (32-bit offsets within an adapter: N <= 2^22, r <= 64)
+    uint32_t boff[C::NI], soff[C::MI];
 #pragma unroll
-    for (int ni = 0; ni < C::NI; ++ni) brow[ni] = p.lout + (int64_t)min(c0 + (wn * C::NI + ni) * 16 + (l & 15), p.NC - 1) * p.lr;
-    while (any) {
+    for (int ni = 0; ni < C::NI; ++ni) boff[ni] = (uint32_t)min(c0 + (wn * C::NI + ni) * 16 + (l & 15), p.NC - 1) * p.lr;
+#pragma unroll
+    for (int mi = 0; mi < C::MI; ++mi) soff[mi] = (uint32_t)min((wm * C::MI + mi) * 16 + (l & 15), rt.rows - 1) * p.lr;
+    const lora_bf16* s0 = p.ltok + (int64_t)rt.row_start * p.lr;
+    auto next = [&]() {                                      // an adapter whose rows are still to come; -1: none
         int g = -1;
-        any = 0;
 #pragma unroll
         for (int mi = 0; mi < C::MI; ++mi) {
             if (g < 0 && todo[mi]) g = __builtin_amdgcn_readlane(id[mi], __builtin_ctz(todo[mi]));
-            todo[mi] &= ~(uint32_t)__ballot(id[mi] == g);
-            any |= todo[mi];
+            if (g >= 0) todo[mi] &= ~(uint32_t)__ballot(id[mi] == g);
         }
-        const int rank = p.ranks ? min(p.ranks[g], p.lr) : p.lr;
-        for (int kk = 0; kk * 32 < rank; ++kk) {
-            const int k = 32 * kk + 8 * (l >> 4), left = rank - k;      // entries of this lane's eight that the adapter has
-            u32x4 b[C::NI];
+        return g;
+    };
+    const bool paired = p.lr == 16;
+    int g = any ? next() : -1, part = 0;                     // what comes next, and (rank 64) its second half
+    while (g >= 0) {
+        u32x4 b[BATCH][C::NI], s[BATCH][C::MI];
+        int steps = 0;
 #pragma unroll
-            for (int ni = 0; ni < C::NI; ++ni) {
-                b[ni] = u32x4{0u, 0u, 0u, 0u};
-                if (left > 0) b[ni] = *(const u32x4*)(brow[ni] + (int64_t)g * p.NC * p.lr + k);
+        for (int t = 0; t < BATCH; ++t) {
+#pragma unroll
+            for (int ni = 0; ni < C::NI; ++ni) b[t][ni] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int mi = 0; mi < C::MI; ++mi) s[t][mi] = u32x4{0u, 0u, 0u, 0u};
+            if (g < 0) continue;
+            steps = t + 1;
+            int mine = g, k = 32 * part + 8 * q;             // this lane's adapter and first column of the rank
+            if (paired) {
+                const int other = next();
+                if (q >= 2) {
+                    mine = other;
+                    k -= 16;
+                }
+                g = next();
+            } else if (part == 0 && p.lr == 64) {
+                part = 1;
+            } else {
+                part = 0;
+                g = next();
             }
-            if (left > 0 && left < 8)
+            if (mine < 0) continue;
+            const int left = (p.ranks ? min(p.ranks[mine], p.lr) : p.lr) - k;      // entries of this lane's eight that the adapter has
+            if (left <= 0) continue;
+            const lora_bf16* bg = p.lout + (int64_t)mine * p.NC * p.lr + k;
+#pragma unroll
+            for (int ni = 0; ni < C::NI; ++ni) b[t][ni] = *(const u32x4*)(bg + boff[ni]);
+            if (left < 8)
 #pragma unroll
                 for (int ni = 0; ni < C::NI; ++ni)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) b[ni][i] &= 2 * i + 1 < left ? 0xFFFFFFFFu : 2 * i < left ? 0xFFFFu : 0u;
+                    for (int i = 0; i < 4; ++i) b[t][ni][i] &= 2 * i + 1 < left ? 0xFFFFFFFFu : 2 * i < left ? 0xFFFFu : 0u;
 #pragma unroll
-            for (int mi = 0; mi < C::MI; ++mi) {
-                if (__ballot(id[mi] == g) == 0) continue;
-                u32x4 s = u32x4{0u, 0u, 0u, 0u};
-                if (left > 0 && id[mi] == g) s = *(const u32x4*)(p.ltok + (int64_t)(rt.row_start + (wm * C::MI + mi) * 16 + (l & 15)) * p.lr + k);
+            for (int mi = 0; mi < C::MI; ++mi)
+                if (id[mi] == mine) s[t][mi] = *(const u32x4*)(s0 + soff[mi] + k);
+        }
+#pragma unroll
+        for (int t = 0; t < BATCH; ++t) {
+            if (t >= steps) break;
+#pragma unroll
+            for (int mi = 0; mi < C::MI; ++mi)
 #pragma unroll
                 for (int ni = 0; ni < C::NI; ++ni)
-                    acc[mi][ni] = LF_MFMA(__builtin_bit_cast(bf16x8, b[ni]), __builtin_bit_cast(bf16x8, s), acc[mi][ni]);
-            }
+                    acc[mi][ni] = LF_MFMA(__builtin_bit_cast(bf16x8, b[t][ni]), __builtin_bit_cast(bf16x8, s[t][mi]), acc[mi][ni]);
         }
     }
 }

@@ -95,54 +95,54 @@ __global__ void __launch_bounds__(64) request_rows_kernel(RequestDownArgs p) {
     }
 }
 
-// 16 rows to a workgroup, every fourth 64-deep slab of the contraction to a wave; a lane's two 16-byte loads of a row's slab lie side by side.
-template <int RB>
-__global__ void __launch_bounds__(256) request_tile_kernel(RequestDownArgs p) {
-    __shared__ f32x4 red[4][RB][64];
-    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.x * 16 + (l & 15);
+// 16 rows by 16 columns of the rank to a workgroup, every eighth 64-deep slab of the contraction to a wave, four of them under way at
+// once; a lane's two 16-byte loads of a row's slab lie side by side.
+constexpr int kTileWaves = 8;
+__global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestDownArgs p) {
+    __shared__ f32x4 red[kTileWaves][64];
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.x * 16 + (l & 15), j0 = blockIdx.y * 16;
     int id = row < p.M ? p.ids[row] : -1;
     if (id >= p.P) id = -1;
     const lora_bf16* x = p.X + (int64_t)min(row, p.M - 1) * p.K + 16 * (l >> 4);
-    f32x4 all[RB];
-#pragma unroll
-    for (int j = 0; j < RB; ++j) all[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 all = f32x4{0.f, 0.f, 0.f, 0.f};
     uint32_t todo = (uint32_t)__ballot(id >= 0) & 0xFFFFu;
     while (todo) {
         const int g = __builtin_amdgcn_readlane(id, __builtin_ctz(todo));
         todo &= ~(uint32_t)__ballot(id == g);
-        const lora_bf16* a = p.A + ((int64_t)g * p.r + (l & 15)) * p.K + 16 * (l >> 4);
-        f32x4 acc[RB];
+        if (p.ranks && p.ranks[g] <= j0) continue;
+        const lora_bf16* a = p.A + ((int64_t)g * p.r + j0 + (l & 15)) * p.K + 16 * (l >> 4);
+        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        constexpr int U = 4;
+        for (int k = 64 * w; k < p.K; k += 64 * kTileWaves * U) {
+            bf16x8 xf[U][2], af[U][2];
 #pragma unroll
-        for (int j = 0; j < RB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int k = 64 * w; k < p.K; k += 256) {
-            bf16x8 xf[2], af[RB][2];
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                xf[h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(x + k + 8 * h));
+                for (int h = 0; h < 2; ++h) {
+                    const int at = min(k + 64 * kTileWaves * u, p.K - 64) + 8 * h;       // (past the end: brought, not used)
+                    xf[u][h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(x + at));
+                    af[u][h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(a + at));
+                }
 #pragma unroll
-                for (int j = 0; j < RB; ++j) af[j][h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(a + (int64_t)16 * j * p.K + k + 8 * h));
-            }
+            for (int u = 0; u < U; ++u)
+                if (k + 64 * kTileWaves * u < p.K)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < RB; ++j) acc[j] = LF_MFMA(af[j][h], xf[h], acc[j]);
+                    for (int h = 0; h < 2; ++h) acc = LF_MFMA(af[u][h], xf[u][h], acc);
         }
 #pragma unroll
-        for (int j = 0; j < RB; ++j) all[j] = id == g ? acc[j] : all[j];
+        for (int e = 0; e < 4; ++e) all[e] = id == g ? acc[e] : all[e];
     }
-#pragma unroll
-    for (int j = 0; j < RB; ++j) red[w][j][l] = all[j];
+    red[w][l] = all;
     __syncthreads();
-    for (int j = w; j < RB; j += 4) {
-        const f32x4 v = (red[0][j][l] + red[1][j][l]) + (red[2][j][l] + red[3][j][l]);
-        if (row >= p.M) continue;
-        const int c = 16 * j + 4 * (l >> 4), rank = id < 0 ? 0 : p.ranks ? p.ranks[id] : p.r;
-        const float s = id < 0 ? 0.f : p.s[id];
-        float o[4];
+    if (w || row >= p.M) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = c + e < rank ? s * v[e] : 0.f;
-        *(u32x2*)(p.S + (int64_t)row * p.r + c) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
-    }
+    for (int i = 1; i < kTileWaves; ++i) all += red[i][l];
+    const int c = j0 + 4 * (l >> 4), rank = id < 0 ? 0 : p.ranks ? p.ranks[id] : p.r;
+    const float s = id < 0 ? 0.f : p.s[id];
+    float o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = c + e < rank ? s * all[e] : 0.f;
+    *(u32x2*)(p.S + (int64_t)row * p.r + c) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
 }
 
 static hipError_t launch_request_down(const RequestDownArgs& a, hipStream_t st) {
@@ -152,10 +152,7 @@ static hipError_t launch_request_down(const RequestDownArgs& a, hipStream_t st) 
     } else if (a.M <= 512) {
         hipLaunchKernelGGL(request_rows_kernel<4>, dim3((unsigned)(a.M + 3) / 4, parts), dim3(64), 0, st, a);
     } else {
-        const dim3 grid((unsigned)(a.M + 15) / 16), block(256);
-        if (a.r == 16) hipLaunchKernelGGL(request_tile_kernel<1>, grid, block, 0, st, a);
-        else if (a.r == 32) hipLaunchKernelGGL(request_tile_kernel<2>, grid, block, 0, st, a);
-        else hipLaunchKernelGGL(request_tile_kernel<4>, grid, block, 0, st, a);
+        hipLaunchKernelGGL(request_tile_kernel, dim3((unsigned)(a.M + 15) / 16, (unsigned)a.r / 16), dim3(64 * kTileWaves), 0, st, a);
     }
     return hipGetLastError();
 }

@@ -10,6 +10,7 @@
 namespace lf {
 
 constexpr int kRopeThreads = 256;
+constexpr int kRopeBlocks = 4 * kComputeUnits;      // of the backward: each leaves a plane of partial sums, so no more than fill the chip
 
 // GL lanes to a head, a wave for a row, or for a part of its heads.
 template <int GL, bool INTER>
@@ -82,6 +83,8 @@ template <int GL>
 struct RopePasses {
     static constexpr int HEADS = 64 / GL;
     int of_q, all;
+    // first of the keys' passes that part `part` takes
+    __device__ __forceinline__ int first_k(int part, int parts) const { const int r = (part - of_q) % parts; return r < 0 ? r + parts : r; }
     __host__ __device__ RopePasses(int H, int G) : of_q((H + HEADS - 1) / HEADS), all((H + HEADS - 1) / HEADS + (G + HEADS - 1) / HEADS) {}
 };
 
@@ -107,42 +110,43 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
         fold(p.gamma_q, cq, sq);
         fold(p.gamma_k, ck, sk);
     }
-    constexpr int U = 4;                                   // passes whose loads are in flight together
-    for (int first = (int)(unit % p.parts); first < ps.all; first += U * p.parts) {
-        u32x4 raw[U];
-        bool ok[U];
+    auto heads = [&](const lora_bf16* x_row, lora_bf16* out_row, int n, int passes, int first, const float (&cg)[8], const float (&sg)[8]) {
+        constexpr int U = 4;                               // passes whose loads are in flight together
+        for (; first < passes; first += U * p.parts) {
+            u32x4 raw[U];
+            bool ok[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int pass = first + u * p.parts;
-            const bool is_q = pass < ps.of_q;
-            const int head = (is_q ? pass : pass - ps.of_q) * ps.HEADS + ln.slot;
-            ok[u] = pass < ps.all && ln.active && head < (is_q ? p.H : p.G);
-            raw[u] = u32x4{0u, 0u, 0u, 0u};
-            if (ok[u]) raw[u] = *(const u32x4*)((is_q ? p.q + row * p.ldq : p.k + row * p.ldk) + (int64_t)head * p.D + 8 * ln.j);
+            for (int u = 0; u < U; ++u) {
+                const int head = (first + u * p.parts) * ps.HEADS + ln.slot;
+                ok[u] = ln.active && head < n;
+                raw[u] = u32x4{0u, 0u, 0u, 0u};
+                if (ok[u]) raw[u] = *(const u32x4*)(x_row + (int64_t)head * p.D + 8 * ln.j);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int pass = first + u * p.parts;
+                if (pass >= passes) break;
+                float x[8], o[8], y[8], sum = 0.f;
+                unpack8(raw[u], x);
+                others(ln, raw[u], o);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
+                const float inv = 1.f / sqrtf(sum_over_head<GL>(sum) / (float)p.D + p.eps);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = inv * (x[i] * cg[i] + o[i] * sg[i]);
+                u32x4 out = pack8(y);
+                if (!known) out = u32x4{0u, 0u, 0u, 0u};
+                if (ok[u]) *(u32x4*)(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j) = out;
+            }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int pass = first + u * p.parts;
-            if (pass >= ps.all) break;
-            const bool is_q = pass < ps.of_q;
-            const int head = (is_q ? pass : pass - ps.of_q) * ps.HEADS + ln.slot;
-            float x[8], o[8], y[8], sum = 0.f;
-            unpack8(raw[u], x);
-            others(ln, raw[u], o);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
-            const float inv = 1.f / sqrtf(sum_over_head<GL>(sum) / (float)p.D + p.eps);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = inv * (x[i] * (is_q ? cq[i] : ck[i]) + o[i] * (is_q ? sq[i] : sk[i]));
-            u32x4 out = pack8(y);
-            if (!known) out = u32x4{0u, 0u, 0u, 0u};
-            if (ok[u]) *(u32x4*)((is_q ? p.q_out + row * p.ldqo : p.k_out + row * p.ldko) + (int64_t)head * p.D + 8 * ln.j) = out;
-        }
-    }
+    };
+    const int part = (int)(unit % p.parts);
+    heads(p.q + row * p.ldq, p.q_out + row * p.ldqo, p.H, ps.of_q, part, cq, sq);
+    heads(p.k + row * p.ldk, p.k_out + row * p.ldko, p.G, ps.all - ps.of_q, ps.first_k(part, p.parts), ck, sk);
 }
 
 template <int GL, bool INTER>
-__global__ void __launch_bounds__(kRopeThreads) rope_bwd_kernel(RopeArgs p) {
+__global__ void __launch_bounds__(kRopeThreads, GL == 32 ? 3 : 4) rope_bwd_kernel(RopeArgs p) {
     __shared__ float red[kRopeThreads / 64][2][GL * 8];
     const RopeLane<GL, INTER> ln(p.D, p.rot);
     const RopePasses<GL> ps(p.H, p.G);
@@ -159,54 +163,54 @@ __global__ void __launch_bounds__(kRopeThreads) rope_bwd_kernel(RopeArgs p) {
         const bool known = pos >= 0 && pos < p.positions;
         float c[8], s[8];
         angles(p, ln, pos, known, c, s);
-        constexpr int U = 2;
-        for (int first = (int)(unit % p.parts); first < ps.all; first += U * p.parts) {
-            u32x4 xr[U], dr[U];
-            bool ok[U];
+        auto heads = [&](const lora_bf16* x_row, const lora_bf16* dy_row, lora_bf16* out_row, int n, int passes, int first, const float (&g)[8],
+                         float (&dg)[8]) {
+            constexpr int U = 2;
+            for (; first < passes; first += U * p.parts) {
+                u32x4 xr[U], dr[U];
+                bool ok[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int pass = first + u * p.parts;
-                const bool is_q = pass < ps.of_q;
-                const int head = (is_q ? pass : pass - ps.of_q) * ps.HEADS + ln.slot;
-                ok[u] = pass < ps.all && ln.active && head < (is_q ? p.H : p.G);
-                xr[u] = dr[u] = u32x4{0u, 0u, 0u, 0u};
-                if (ok[u]) {
-                    xr[u] = *(const u32x4*)((is_q ? p.q + row * p.ldq : p.k + row * p.ldk) + (int64_t)head * p.D + 8 * ln.j);
-                    if (known) dr[u] = *(const u32x4*)((is_q ? p.dq_out + row * p.lddq : p.dk_out + row * p.lddk) + (int64_t)head * p.D + 8 * ln.j);
+                for (int u = 0; u < U; ++u) {
+                    const int head = (first + u * p.parts) * ps.HEADS + ln.slot;
+                    ok[u] = ln.active && head < n;
+                    xr[u] = dr[u] = u32x4{0u, 0u, 0u, 0u};
+                    if (ok[u]) {
+                        xr[u] = *(const u32x4*)(x_row + (int64_t)head * p.D + 8 * ln.j);
+                        if (known) dr[u] = *(const u32x4*)(dy_row + (int64_t)head * p.D + 8 * ln.j);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int pass = first + u * p.parts;
+                    if (pass >= passes) break;
+                    float x[8], e[8], o[8], sxx = 0.f, sux = 0.f;
+                    unpack8(xr[u], x);
+                    unpack8(dr[u], e);
+                    others(ln, dr[u], o);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        e[i] = e[i] * c[i] - o[i] * s[i];
+                        sxx += x[i] * x[i];
+                        sux += e[i] * g[i] * x[i];
+                    }
+                    sxx = sum_over_head<GL>(sxx);
+                    sux = sum_over_head<GL>(sux);
+                    const float inv = 1.f / sqrtf(sxx / (float)p.D + p.eps), back = inv * inv * sux / (float)p.D;
+                    float dx[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        dg[i] += e[i] * x[i] * inv;
+                        dx[i] = inv * (e[i] * g[i] - x[i] * back);
+                    }
+                    u32x4 out = pack8(dx);
+                    if (!known) out = u32x4{0u, 0u, 0u, 0u};
+                    if (ok[u]) *(u32x4*)(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j) = out;
                 }
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int pass = first + u * p.parts;
-                if (pass >= ps.all) break;
-                const bool is_q = pass < ps.of_q;
-                const int head = (is_q ? pass : pass - ps.of_q) * ps.HEADS + ln.slot;
-                float x[8], e[8], o[8], sxx = 0.f, sux = 0.f;
-                unpack8(xr[u], x);
-                unpack8(dr[u], e);
-                others(ln, dr[u], o);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    e[i] = e[i] * c[i] - o[i] * s[i];
-                    sxx += x[i] * x[i];
-                    sux += e[i] * (is_q ? gq[i] : gk[i]) * x[i];
-                }
-                sxx = sum_over_head<GL>(sxx);
-                sux = sum_over_head<GL>(sux);
-                const float inv = 1.f / sqrtf(sxx / (float)p.D + p.eps), back = inv * inv * sux / (float)p.D;
-                float dx[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float n = e[i] * x[i] * inv;
-                    if (is_q) dgq[i] += n;
-                    else dgk[i] += n;
-                    dx[i] = inv * (e[i] * (is_q ? gq[i] : gk[i]) - x[i] * back);
-                }
-                u32x4 out = pack8(dx);
-                if (!known) out = u32x4{0u, 0u, 0u, 0u};
-                if (ok[u]) *(u32x4*)((is_q ? p.q_out + row * p.ldqo : p.k_out + row * p.ldko) + (int64_t)head * p.D + 8 * ln.j) = out;
-            }
-        }
+        };
+        const int part = (int)(unit % p.parts);
+        heads(p.q + row * p.ldq, p.dq_out + row * p.lddq, p.q_out + row * p.ldqo, p.H, ps.of_q, part, gq, dgq);
+        heads(p.k + row * p.ldk, p.dk_out + row * p.lddk, p.k_out + row * p.ldko, p.G, ps.all - ps.of_q, ps.first_k(part, p.parts), gk, dgk);
     }
     // over the heads of the wave, then over the waves, in a fixed order
 #pragma unroll
@@ -228,19 +232,30 @@ __global__ void __launch_bounds__(kRopeThreads) rope_bwd_kernel(RopeArgs p) {
     }
 }
 
-// dgamma (+)= the sum over the blocks' planes: 16 columns to a workgroup, 16 threads to a column, each with every 16th plane.
+// dgamma (+)= the sum over the blocks' planes: eight columns to a workgroup, two threads to a plane, each of them with every 128th.  All loads of
+// a thread are under way together: with 16 workgroups of 16 columns, whose threads went through 64 planes one by one, 1024 planes took 20 us.
 __global__ void __launch_bounds__(256) rope_finalize_kernel(RopeFinalizeArgs p) {
-    __shared__ float red[16][17];
-    const int cl = threadIdx.x & 15, sl = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
-    float v = 0.f;
-    for (int b = sl; b < p.blocks; b += 16) v += p.part[(int64_t)b * 2 * p.D + c];
-    red[sl][cl] = v;
-    __syncthreads();
-    if (sl) return;
+    __shared__ f32x4 red[128][2];
+    const int half = threadIdx.x & 1, sl = threadIdx.x >> 1, c = blockIdx.x * 8 + 4 * half;
+    f32x4 v[kRopeBlocks / 128];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) v += red[i][cl];
+    for (int i = 0; i < kRopeBlocks / 128; ++i) {
+        v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (sl + 128 * i < p.blocks) v[i] = *(const f32x4*)(p.part + (int64_t)(sl + 128 * i) * 2 * p.D + c);
+    }
+#pragma unroll
+    for (int i = 1; i < kRopeBlocks / 128; ++i) v[0] += v[i];
+    red[sl][half] = v[0];
+#pragma unroll
+    for (int n = 64; n > 0; n >>= 1) {
+        __syncthreads();
+        if (sl < n) red[sl][half] += red[sl + n][half];
+    }
+    if (sl) return;
+    v[0] = red[0][half];
     float* out = c < p.D ? p.dgamma_q + c : p.dgamma_k + c - p.D;
-    *out = p.accumulate ? *out + v : v;
+    if (p.accumulate) v[0] += *(const f32x4*)out;
+    *(f32x4*)out = v[0];
 }
 
 // Parts of a row while there are fewer rows than 16 waves to a compute unit, but no more than its passes.
@@ -267,8 +282,6 @@ hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st) {
     });
 }
 
-// Every block leaves a plane of partial sums, so no more of them than fill the chip.
-constexpr int kRopeBlocks = 4 * kComputeUnits;
 int rope_blocks(int64_t M, int H, int G, int D) {
     return with_lanes(D, [&](auto gl) {
         const int64_t n = (M * rope_parts<gl()>(M, H, G) + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
@@ -286,7 +299,7 @@ hipError_t launch_rope_bwd(RopeArgs a, bool interleaved, const RopeFinalizeArgs&
         });
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(rope_finalize_kernel, dim3(2 * a.D / 16), dim3(256), 0, st, f);
+    hipLaunchKernelGGL(rope_finalize_kernel, dim3(2 * a.D / 8), dim3(256), 0, st, f);
     return hipGetLastError();
 }
 

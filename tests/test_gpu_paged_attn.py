@@ -161,6 +161,27 @@ def test_not_finite_query_stays_in_its_row():
         assert torch.equal(bad, want)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("n,kv,H,G,D,window", [(4, 50, 4, 2, 64, 0), (12, 70, 2, 1, 128, 0), (20, 90, 2, 2, 128, 6), (90, 200, 4, 2, 64, 0), (100, 130, 2, 1, 128, 0),
+                                               (130, 300, 2, 2, 128, 40), (1, 90, 8, 2, 128, 20)])
+def test_not_finite_keys_and_values_reach_only_rows_that_see_them(n, kv, H, G, D, window, fp8):
+    q, cache, table, offsets, lens, held = _setup([(n, kv)], H, G, D, 16, fp8, n + D)
+    k, v = (x.clone() for x in held[0])
+    for j, (x, val) in enumerate(((v, float("inf")), (v, NAN), (v, -float("inf")), (k, NAN), (v, NAN))):
+        at, g, d = kv - 1 - (j * n) // 6, j % G, 5 + 11 * j
+        val = NAN if fp8 else val
+        x[at, g, d] = val
+        page, row = int(table[0, at // 16]), at % 16
+        t = cache.tensors[0 if x is k else 1]
+        if fp8:
+            t.view(torch.uint8)[page, g, row, d] = 0x7F
+        else:
+            t[page, g, row, d] = val
+    out = binding.lora_paged_attn_fwd(q.cuda(), cache, table.cuda(), offsets.cuda(), lens.cuda(), n, kv, window=window)
+    ref, bound = attention(q.to(F64), k, v, n, kv, D ** -0.5, window)
+    within(out, ref, bound, (n, kv, D, window, fp8))
+
+
 def test_arguments():
     q, cache, table, offsets, lens, _ = _setup([(2, 30)], 4, 2, 64, 16, False, 1)
     q, table, offsets, lens = (t.cuda() for t in (q, table, offsets, lens))
