@@ -298,7 +298,7 @@ lora_status lora_ceiling_hbm_read(const void* src, size_t bytes, uint32_t* sink,
  * X [M,K]  W [N,K]  A [P,r,K]  B [P,N,r]  Y [M,N];  device arrays ids [M], s [P], ranks [P].  ranks (may be NULL: all r): adapter g
  * uses the first ranks[g] rows of A[g] and columns of B[g], any number of 0 .. r (values outside are cut to it); the others may
  * hold anything.  S [M,r]: scratch that receives s (X A^T), zero past the rank.  No dropout: a row's result is that of lora_fwd
- * with p = 0 up to rounding of S.  M < 2^31, K, N, r as above; any P >= 1; adapters may come in any order and number. */
+ * with p = 0 up to the order of the sums in S.  M < 2^21, K, N, r as above; any P >= 1; adapters may come in any order and number. */
 lora_status lora_requests_fwd(const lora_bf16* X, const lora_bf16* W, const lora_bf16* A, const lora_bf16* B, const int32_t* ids,
                               const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P, lora_bf16* Y,
                               lora_bf16* S, lora_stream stream);

@@ -293,97 +293,116 @@ __device__ __forceinline__ void ring_stage(f32x4 (&acc)[C::MI][C::NI], const Rin
     }
 }
 
-// LoRA term of rows with an adapter each, on the accumulators of the wave's MI x NI blocks: a matrix step for every adapter among its rows
-// (two at rank 64; at rank 16 two adapters share one, each on half of the contraction), with the other rows' S left out, so that no value
-// of one adapter meets a row of another, not even multiplied by zero.  S and B come straight from memory in the fragments' layout:
-// an adapter's few rows are read once, and by this wave alone.  The operands of BATCH steps are under way together, or each
-// step would wait for memory by itself.
+// LoRA term of rows with an adapter each, on the accumulators of the wave's MI x NI blocks: a matrix step for every adapter among its rows and
+// every 32 columns of its rank (of rank 16 two adapters share a step, each on half of the contraction), with the other rows' S left
+// out, so that no value of one adapter meets a row of another, not even multiplied by zero.  S and B come straight from memory in
+// the fragments' layout: an adapter's few rows are read once, and by this wave alone.  The steps stand in a list in LDS, and their operands
+// are asked for DEPTH steps ahead.  The first of them before the base product, where the registers can hold them through it (LATE; the small
+// tiles: 16 rows to a wave): they come in meanwhile.  Elsewhere the whole term comes before the base product, while the copying waves fill the
+// ring.  us, rows with 64 adapters in turn, r = 16 (and with none), against the same after the base product with every batch of steps waited for: 200
+// rows, 4096 -> 14336 69 (46) / 74 (47); 2048 rows, 4096 -> 4096 96 (60) / 201 (62, the first product's 84 us among it); 64 rows, 4096 -> 6144 20
+// (14) / 19 (14).  200 rows with 106 adapters of mean rank 37, 4096 -> 14336, this launch alone 91 / 132.
 template <class C>
-__device__ __forceinline__ void request_term(const RingRequestArgs& p, f32x4 (&acc)[C::MI][C::NI], const RowTile& rt, int c0, int wm, int wn) {
-    // what the registers hold beside the accumulators and some forty others, with two workgroups on a compute unit where the rings allow two
-    constexpr int WAVES = (C::NW + C::CW) * (2 * C::LDS <= 160 * 1024 ? 2 : 1), HOLD = 512 / ((WAVES + 3) / 4) / 8 * 8;
-    constexpr int FIT = (HOLD - C::MI * C::NI * 4 - 45) / ((C::MI + C::NI) * 4), BATCH = FIT < 1 ? 1 : FIT > 8 ? 8 : FIT;
-    const int l = threadIdx.x & 63, q = l >> 4;
-    int id[C::MI];
-    uint32_t todo[C::MI];                                    // rows (bits) of a block whose adapter is still to come
-    bool any = false;
-#pragma unroll
-    for (int mi = 0; mi < C::MI; ++mi) {
-        const int row = (wm * C::MI + mi) * 16 + (l & 15);
-        id[mi] = p.ids[rt.row_start + min(row, rt.rows - 1)];
-        if (row >= rt.rows || id[mi] >= p.P) id[mi] = -1;
-        todo[mi] = (uint32_t)__ballot(id[mi] >= 0) & 0xFFFFu;
-        any |= todo[mi] != 0;
-    }
-    // (32-bit offsets within an adapter: N <= 2^22, r <= 64)
-    uint32_t boff[C::NI], soff[C::MI];
-#pragma unroll
-    for (int ni = 0; ni < C::NI; ++ni) boff[ni] = (uint32_t)min(c0 + (wn * C::NI + ni) * 16 + (l & 15), p.NC - 1) * p.lr;
-#pragma unroll
-    for (int mi = 0; mi < C::MI; ++mi) soff[mi] = (uint32_t)min((wm * C::MI + mi) * 16 + (l & 15), rt.rows - 1) * p.lr;
-    const lora_bf16* s0 = p.ltok + (int64_t)rt.row_start * p.lr;
-    auto next = [&]() {                                      // an adapter whose rows are still to come; -1: none
-        int g = -1;
-#pragma unroll
-        for (int mi = 0; mi < C::MI; ++mi) {
-            if (g < 0 && todo[mi]) g = __builtin_amdgcn_readlane(id[mi], __builtin_ctz(todo[mi]));
-            if (g >= 0) todo[mi] &= ~(uint32_t)__ballot(id[mi] == g);
-        }
-        return g;
-    };
-    const bool paired = p.lr == 16;
-    int g = any ? next() : -1, part = 0;                     // what comes next, and (rank 64) its second half
-    while (g >= 0) {
-        u32x4 b[BATCH][C::NI], s[BATCH][C::MI];
-        int steps = 0;
-#pragma unroll
-        for (int t = 0; t < BATCH; ++t) {
-#pragma unroll
-            for (int ni = 0; ni < C::NI; ++ni) b[t][ni] = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int mi = 0; mi < C::MI; ++mi) s[t][mi] = u32x4{0u, 0u, 0u, 0u};
-            if (g < 0) continue;
-            steps = t + 1;
-            int mine = g, k = 32 * part + 8 * q;             // this lane's adapter and first column of the rank
-            if (paired) {
-                const int other = next();
-                if (q >= 2) {
-                    mine = other;
-                    k -= 16;
-                }
-                g = next();
-            } else if (part == 0 && p.lr == 64) {
-                part = 1;
-            } else {
-                part = 0;
-                g = next();
+struct RequestList {                                          // of a wave
+    static constexpr int ROWS = C::MI * 16;
+    int id[ROWS];                                             // adapter of each row, -1: none
+    u32x2 unit[2 * ROWS];                                     // adapter; its rank and, in the upper half, the first of the unit's columns
+};
+template <class C>
+struct RequestTerm {
+    static constexpr int MI = C::MI, NI = C::NI, ROWS = MI * 16;
+    static_assert(ROWS <= 64, "a lane for every row");
+    // what the registers hold beside the accumulators and some forty others (LATE: and the fragments of the base product), with two workgroups on
+    // a compute unit where the rings allow two (32 x 32 tiles are taken while each has one for itself).  Not more where the launch leaves a
+    // workgroup by itself: eight steps ahead instead of four measured the same.
+    static constexpr int WAVES = (C::NW + C::CW) * (2 * C::LDS <= 160 * 1024 && C::TN > 32 ? 2 : 1), HOLD = 512 / ((WAVES + 3) / 4) / 8 * 8;
+    static constexpr int FRAGS = (C::AHEAD ? 2 * C::SUBS : 2) * (MI + NI) * 4;
+    static constexpr int fit(int beside) { return (HOLD - MI * NI * 4 - 40 - beside) / ((MI + NI) * 4); }
+    static constexpr bool LATE = fit(FRAGS) >= 4;
+    static constexpr int FIT = fit(LATE ? FRAGS : 0), DEPTH = FIT < 1 ? 1 : FIT > 8 ? 8 : FIT;
+
+    const RingRequestArgs& p;
+    const RequestList<C>& list;
+    const lora_bf16* s0;
+    int n = 0, steps = 0;                                     // units, steps
+    int id[MI];
+    uint32_t boff[NI], soff[MI];                              // (32-bit offsets within an adapter: N <= 2^22, r <= 64)
+    u32x4 b[DEPTH][NI], s[DEPTH][MI];
+
+    __device__ __forceinline__ RequestTerm(const RingRequestArgs& args, const RowTile& rt, int c0, int wm, int wn, RequestList<C>& out)
+        : p(args), list(out), s0(args.ltok + (int64_t)rt.row_start * args.lr) {
+        const int l = threadIdx.x & 63, width = p.lr == 16 ? 16 : 32;
+        const int row = wm * ROWS + l;
+        int of = p.ids[rt.row_start + min(row, rt.rows - 1)];
+        if (l >= ROWS || row >= rt.rows || of >= p.P || of < 0) of = -1;
+        const int rank = of < 0 ? 0 : p.ranks ? max(min(p.ranks[of], p.lr), 0) : p.lr;
+        if (l < ROWS) out.id[l] = of;
+        uint64_t todo = __ballot(rank > 0);
+        while (todo) {
+            const int first = __builtin_ctzll(todo), g = __builtin_amdgcn_readlane(of, first), rk = __builtin_amdgcn_readlane(rank, first);
+            todo &= ~__ballot(of == g);
+            for (int k0 = 0; k0 < rk; k0 += width) {
+                if (l == 0) out.unit[n] = u32x2{(uint32_t)g, (uint32_t)(rk | k0 << 16)};
+                ++n;
             }
-            if (mine < 0) continue;
-            const int left = (p.ranks ? min(p.ranks[mine], p.lr) : p.lr) - k;      // entries of this lane's eight that the adapter has
-            if (left <= 0) continue;
-            const lora_bf16* bg = p.lout + (int64_t)mine * p.NC * p.lr + k;
+        }
+        steps = width == 16 ? (n + 1) / 2 : n;
+        asm volatile("" ::: "memory");                        // (LDS operations of a wave complete in order)
 #pragma unroll
-            for (int ni = 0; ni < C::NI; ++ni) b[t][ni] = *(const u32x4*)(bg + boff[ni]);
-            if (left < 8)
-#pragma unroll
-                for (int ni = 0; ni < C::NI; ++ni)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) b[t][ni][i] &= 2 * i + 1 < left ? 0xFFFFFFFFu : 2 * i < left ? 0xFFFFu : 0u;
-#pragma unroll
-            for (int mi = 0; mi < C::MI; ++mi)
-                if (id[mi] == mine) s[t][mi] = *(const u32x4*)(s0 + soff[mi] + k);
+        for (int mi = 0; mi < MI; ++mi) {
+            id[mi] = list.id[mi * 16 + (l & 15)];
+            soff[mi] = (uint32_t)min(wm * ROWS + mi * 16 + (l & 15), rt.rows - 1) * p.lr;
         }
 #pragma unroll
-        for (int t = 0; t < BATCH; ++t) {
-            if (t >= steps) break;
+        for (int ni = 0; ni < NI; ++ni) boff[ni] = (uint32_t)min(c0 + (wn * NI + ni) * 16 + (l & 15), p.NC - 1) * p.lr;
 #pragma unroll
-            for (int mi = 0; mi < C::MI; ++mi)
+        for (int t = 0; t < DEPTH; ++t) ask(t, t);
+    }
+
+    // The operands of a step, into place t.
+    __device__ __forceinline__ void ask(int step, int t) {
+        const int q = (threadIdx.x & 63) >> 4;
+        const bool paired = p.lr == 16;
 #pragma unroll
-                for (int ni = 0; ni < C::NI; ++ni)
-                    acc[mi][ni] = LF_MFMA(__builtin_bit_cast(bf16x8, b[t][ni]), __builtin_bit_cast(bf16x8, s[t][mi]), acc[mi][ni]);
+        for (int ni = 0; ni < NI; ++ni) b[t][ni] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) s[t][mi] = u32x4{0u, 0u, 0u, 0u};
+        const int u = paired ? 2 * step + (q >> 1) : step;
+        if (u >= n) return;
+        const u32x2 e = list.unit[u];
+        const int g = (int)e.x, k = (int)(e.y >> 16) + (paired ? 8 * (q & 1) : 8 * q), left = (int)(e.y & 0xFFFFu) - k;
+        if (left <= 0) return;                                // entries of this lane's eight that the adapter has
+        const lora_bf16* bg = p.lout + (int64_t)g * p.NC * p.lr + k;
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) b[t][ni] = *(const u32x4*)(bg + boff[ni]);
+        if (left < 8)
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[t][ni][i] &= 2 * i + 1 < left ? 0xFFFFFFFFu : 2 * i < left ? 0xFFFFu : 0u;
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+            if (id[mi] == g) s[t][mi] = *(const u32x4*)(s0 + soff[mi] + k);
+    }
+
+    __device__ __forceinline__ void add(f32x4 (&acc)[MI][NI]) {
+        for (int step = 0; step < steps; step += DEPTH) {
+#pragma unroll
+            for (int t = 0; t < DEPTH; ++t) {
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int ni = 0; ni < NI; ++ni)
+                        acc[mi][ni] = LF_MFMA(__builtin_bit_cast(bf16x8, b[t][ni]), __builtin_bit_cast(bf16x8, s[t][mi]), acc[mi][ni]);
+                if (step + t + DEPTH < steps) ask(step + t + DEPTH, t);
+                else
+#pragma unroll
+                    for (int ni = 0; ni < NI; ++ni) b[t][ni] = u32x4{0u, 0u, 0u, 0u};
+            }
         }
     }
-}
+};
+struct NoRequests {};
 
 template <class C, bool COL, class Args>
 __device__ __forceinline__ void ring_tile(const Args& p, char* smem) {
@@ -451,6 +470,14 @@ __device__ __forceinline__ void ring_tile(const Args& p, char* smem) {
     for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr bool REQUESTS = std::is_same_v<Args, RingRequestArgs>;
+    auto term_of = [&]() {
+        if constexpr (REQUESTS) return RequestTerm<C>(p, rt, c0, wm, wn, ((RequestList<C>*)(smem + C::LDS))[w]);
+        else return NoRequests{};
+    };
+    auto requests = term_of();
+    if constexpr (REQUESTS)
+        if constexpr (!RequestTerm<C>::LATE) requests.add(acc);
 
     asm volatile("s_barrier" ::: "memory");
 
@@ -504,10 +531,7 @@ __device__ __forceinline__ void ring_tile(const Args& p, char* smem) {
 
     // LoRA term: (2) on the same accumulators; (5) by itself, masked and added
     const int rank_chunks = has_lora ? p.tb.a[rt.g].rank >> 3 : 0;
-    if constexpr (std::is_same_v<Args, RingRequestArgs>) {
-        ring_mfma_done<MI, NI>(acc);
-        request_term<C>(p, acc, rt, c0, wm, wn);
-    } else if (has_lora) {
+    if (has_lora) {
         // block rows of the tile from row `first` on into `to`; the fragments of sub-step 0 are in f0
         auto term = [&](auto& to, auto first) {
             constexpr int FIRST = first(), ROWS = sizeof(to) / sizeof(to[0]);
@@ -550,6 +574,8 @@ __device__ __forceinline__ void ring_tile(const Args& p, char* smem) {
         }
     } else {
         ring_mfma_done<MI, NI>(acc);
+        if constexpr (REQUESTS)
+            if constexpr (RequestTerm<C>::LATE) requests.add(acc);
     }
 
     // Way out: the bf16 tile goes through LDS (rows of TN * 2 bytes, eight-byte slots XOR-ed so that the 16 rows x 2
@@ -679,7 +705,7 @@ static auto with_ring(int kind, const Args& a, F&& f) {
         case 0: return f(Ring<128, 256, 2, 4, 3, 0, 4>{}, a);
         case 1: return f(Ring<128, 128, 2, 2, 4, 2, 2>{}, a);
         case 2: return f(Ring<64, 128, 2, 4, 3, 1, 2>{}, a);
-        case 3: return f(Ring<64, 64, 2, 2, COL ? 4 : 5, 2, 2>{}, a);
+        case 3: return f(Ring<64, 64, 2, 2, COL || std::is_same_v<Args, RingRequestArgs> ? 4 : 5, 2, 2>{}, a);     // (with a wave's list of adapters)
         case 4:
             if (ring_halves(a.tiles_m, a.tiles_n)) {
                 Args h = a;
@@ -731,13 +757,15 @@ hipError_t launch_ring(int kind, bool col, const RingArgs& a, hipStream_t st) {
 
 template <class C>
 static hipError_t launch_requests_cfg(const RingRequestArgs& a, hipStream_t st) {
+    constexpr int LDS = C::LDS + C::NW * (int)sizeof(RequestList<C>);
+    static_assert(LDS <= 160 * 1024, "a compute unit's LDS");
     static bool attr_set = false;                  // one flag per instantiation
     if (!attr_set) {
-        hipError_t e = hipFuncSetAttribute((const void*)ring_requests_kernel<C>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+        hipError_t e = hipFuncSetAttribute((const void*)ring_requests_kernel<C>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
         if (e != hipSuccess) return e;
         attr_set = true;
     }
-    hipLaunchKernelGGL(ring_requests_kernel<C>, dim3((unsigned)((int64_t)a.tiles_m * a.tiles_n)), dim3(C::THREADS + 64 * C::CW), C::LDS, st, a);
+    hipLaunchKernelGGL(ring_requests_kernel<C>, dim3((unsigned)((int64_t)a.tiles_m * a.tiles_n)), dim3(C::THREADS + 64 * C::CW), LDS, st, a);
     return hipGetLastError();
 }
 

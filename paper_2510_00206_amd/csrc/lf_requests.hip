@@ -1,9 +1,8 @@
 // The LoRA linear layer for many requests at once: every row names its adapter, or none, in an array on the device.
 //     S[i] = s_g X[i] A_g^T        this file        (bf16, columns past the adapter's rank zero)
 //     Y[i] = X[i] W^T + S[i] B_g^T  lf_gemm_ring.hip (the small GEMM tiles; the second term on the accumulators: request_term)
-// The first is bound by the reading of the adapters: up to a few hundred rows, which may all have adapters of their own, a wave takes four
-// columns of the rank for one row or for four rows, which share what they read of A if they share the adapter.  More rows come as
-// chunks of few requests: 16 rows to a workgroup by MFMAs, once for every adapter among them.
+// The first is bound by the reading of the adapters: a wave takes four columns of the rank for one row, so that a decode step of a few rows
+// is spread over the chip, or, where many rows come as chunks of few requests, 16 rows go through MFMAs at once.
 #include "lf_gemm_parts.h"
 #include "lf_gemm_ring.h"
 #include "lf_serve.h"
@@ -33,85 +32,65 @@ __device__ __forceinline__ float sum_of_wave(float v) {
 
 constexpr int kDownColumns = 4;                    // columns of the rank to a wave
 
-template <int ROWS>
-__global__ void __launch_bounds__(64) request_rows_kernel(RequestDownArgs p) {
+// Columns j0 .. j0 + 3 of one row of S, by a wave.
+__device__ __forceinline__ void request_row(const RequestDownArgs& p, int row, int j0) {
     constexpr int J = kDownColumns;
-    const int l = threadIdx.x, row0 = blockIdx.x * ROWS, j0 = blockIdx.y * J;
-    int id[ROWS], rank[ROWS];
-    bool shared = true;
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        id[i] = row0 + i < p.M ? p.ids[row0 + i] : -1;
-        if (id[i] >= p.P) id[i] = -1;
-        rank[i] = id[i] < 0 ? 0 : p.ranks ? min(p.ranks[id[i]], p.r) : p.r;
-        shared = shared && id[i] == id[0];
-    }
-    float acc[ROWS][J];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-        for (int j = 0; j < J; ++j) acc[i][j] = 0.f;
-    const u32x4 zero{0u, 0u, 0u, 0u};
-    auto x_at = [&](int i, int k) { return *(const u32x4*)(p.X + (int64_t)(row0 + i) * p.K + k); };
-    auto a_at = [&](int i, int j, int k) { return *(const u32x4*)(p.A + ((int64_t)id[i] * p.r + j0 + j) * p.K + k); };
-    if (shared) {
-        if (rank[0] > j0) {
-#pragma unroll 2
-            for (int k = 8 * l; k < p.K; k += 512) {
-                u32x4 x[ROWS], a[J];
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i) x[i] = row0 + i < p.M ? x_at(i, k) : zero;
-#pragma unroll
-                for (int j = 0; j < J; ++j) a[j] = a_at(0, j, k);
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                    for (int j = 0; j < J; ++j) acc[i][j] = dot8(x[i], a[j], acc[i][j]);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            if (rank[i] <= j0) continue;
+    const int l = threadIdx.x & 63;
+    int id = p.ids[row];
+    if (id >= p.P) id = -1;
+    const int rank = id < 0 ? 0 : p.ranks ? min(p.ranks[id], p.r) : p.r;
+    float v[J] = {};
+    if (rank > j0) {
+        const lora_bf16* x = p.X + (int64_t)row * p.K;
+        const lora_bf16* a = p.A + ((int64_t)id * p.r + j0) * p.K;
 #pragma unroll 4
-            for (int k = 8 * l; k < p.K; k += 512) {
-                const u32x4 x = x_at(i, k);
+        for (int k = 8 * l; k < p.K; k += 512) {
+            const u32x4 xk = *(const u32x4*)(x + k);
 #pragma unroll
-                for (int j = 0; j < J; ++j) acc[i][j] = dot8(x, a_at(i, j, k), acc[i][j]);
-            }
+            for (int j = 0; j < J; ++j) v[j] = dot8(xk, *(const u32x4*)(a + (int64_t)j * p.K + k), v[j]);
         }
-    }
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        if (row0 + i >= p.M) break;
-        const float s = id[i] < 0 ? 0.f : p.s[id[i]];
-        float v[J];
+        const float s = p.s[id];
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            v[j] = sum_of_wave(acc[i][j]);
-            v[j] = j0 + j < rank[i] ? s * v[j] : 0.f;              // (padding of A may hold anything)
+            v[j] = sum_of_wave(v[j]);
+            v[j] = j0 + j < rank ? s * v[j] : 0.f;                 // (padding of A may hold anything)
         }
-        if (l == 0) *(u32x2*)(p.S + (int64_t)(row0 + i) * p.r + j0) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     }
+    if (l == 0) *(u32x2*)(p.S + (int64_t)row * p.r + j0) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
 
-// 16 rows by 16 columns of the rank to a workgroup, every eighth 64-deep slab of the contraction to a wave, four of them under way at
-// once; a lane's two 16-byte loads of a row's slab lie side by side.
+__global__ void __launch_bounds__(64) request_rows_kernel(RequestDownArgs p) { request_row(p, blockIdx.x, blockIdx.y * kDownColumns); }
+
+// Many rows: the 16-row tiles of one adapter by MFMAs, 16 columns of the rank to a workgroup, every eighth 64-deep slab of the contraction to a
+// wave, four of them under way at once (a lane's two 16-byte loads of a row's slab lie side by side).  The rows of the other tiles go to
+// further workgroups of the launch, a wave for each row and four columns, which find nothing to do where the tile is of one adapter.
+// (One after the other in their own workgroups the adapters of such tiles, 37 requests of one token among 2048 rows, took 57 us.)
 constexpr int kTileWaves = 8;
-__global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestDownArgs p) {
+struct RequestTileArgs { RequestDownArgs d; int tiles, parts; };       // parts: of the rank, 16 columns each
+__global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestTileArgs a) {
     __shared__ f32x4 red[kTileWaves][64];
-    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.x * 16 + (l & 15), j0 = blockIdx.y * 16;
-    int id = row < p.M ? p.ids[row] : -1;
-    if (id >= p.P) id = -1;
-    const lora_bf16* x = p.X + (int64_t)min(row, p.M - 1) * p.K + 16 * (l >> 4);
-    f32x4 all = f32x4{0.f, 0.f, 0.f, 0.f};
-    uint32_t todo = (uint32_t)__ballot(id >= 0) & 0xFFFFu;
-    while (todo) {
-        const int g = __builtin_amdgcn_readlane(id, __builtin_ctz(todo));
-        todo &= ~(uint32_t)__ballot(id == g);
-        if (p.ranks && p.ranks[g] <= j0) continue;
-        const lora_bf16* a = p.A + ((int64_t)g * p.r + j0 + (l & 15)) * p.K + 16 * (l >> 4);
-        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    const RequestDownArgs& p = a.d;
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool by_rows = (int)blockIdx.x >= a.tiles * a.parts;
+    // by rows: 4 * parts waves to a row
+    const int unit = by_rows ? ((int)blockIdx.x - a.tiles * a.parts) * kTileWaves + w : 0;
+    const int own = unit / (4 * a.parts), row0 = by_rows ? own & ~15 : (int)blockIdx.x / a.parts * 16;
+    if (row0 >= p.M) return;
+    const int row = row0 + (l & 15);
+    int id = p.ids[min(row, p.M - 1)];
+    if (id < 0 || id >= p.P) id = -1;
+    const int g = __builtin_amdgcn_readfirstlane(id);
+    const bool one = __all(id == g);
+    if (by_rows) {
+        if (!one && own < p.M) request_row(p, own, unit % (4 * a.parts) * kDownColumns);
+        return;
+    }
+    if (!one) return;
+    const int j0 = (int)blockIdx.x % a.parts * 16, rank = g < 0 ? 0 : p.ranks ? min(p.ranks[g], p.r) : p.r;
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (rank > j0) {
+        const lora_bf16* x = p.X + (int64_t)min(row, p.M - 1) * p.K + 16 * (l >> 4);
+        const lora_bf16* ag = p.A + ((int64_t)g * p.r + j0 + (l & 15)) * p.K + 16 * (l >> 4);
         constexpr int U = 4;
         for (int k = 64 * w; k < p.K; k += 64 * kTileWaves * U) {
             bf16x8 xf[U][2], af[U][2];
@@ -121,7 +100,7 @@ __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestDo
                 for (int h = 0; h < 2; ++h) {
                     const int at = min(k + 64 * kTileWaves * u, p.K - 64) + 8 * h;       // (past the end: brought, not used)
                     xf[u][h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(x + at));
-                    af[u][h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(a + at));
+                    af[u][h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(ag + at));
                 }
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -129,31 +108,30 @@ __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestDo
 #pragma unroll
                     for (int h = 0; h < 2; ++h) acc = LF_MFMA(af[u][h], xf[u][h], acc);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) all[e] = id == g ? acc[e] : all[e];
     }
-    red[w][l] = all;
+    red[w][l] = acc;
     __syncthreads();
     if (w || row >= p.M) return;
 #pragma unroll
-    for (int i = 1; i < kTileWaves; ++i) all += red[i][l];
-    const int c = j0 + 4 * (l >> 4), rank = id < 0 ? 0 : p.ranks ? p.ranks[id] : p.r;
-    const float s = id < 0 ? 0.f : p.s[id];
+    for (int i = 1; i < kTileWaves; ++i) acc += red[i][l];
+    const int c = j0 + 4 * (l >> 4);
+    const float s = g < 0 ? 0.f : p.s[g];
     float o[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = c + e < rank ? s * all[e] : 0.f;
+    for (int e = 0; e < 4; ++e) o[e] = c + e < rank ? s * acc[e] : 0.f;
     *(u32x2*)(p.S + (int64_t)row * p.r + c) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
 }
 
+// A wave for every row up to 512 of them, whatever adapters they have, in workgroups of their own, which start sooner than those of eight waves: us, rows /
+// tiles: 3 rows, K = 1024 2.7 / 3.4; 64 rows of 48 adapters, K = 4096, r = 16 4.0 / 6.2; 200 rows of 106 adapters, r = 64 13.8 / 16.5.
 static hipError_t launch_request_down(const RequestDownArgs& a, hipStream_t st) {
-    const unsigned parts = (unsigned)a.r / kDownColumns;
-    if (a.M <= 128) {
-        hipLaunchKernelGGL(request_rows_kernel<1>, dim3((unsigned)a.M, parts), dim3(64), 0, st, a);
-    } else if (a.M <= 512) {
-        hipLaunchKernelGGL(request_rows_kernel<4>, dim3((unsigned)(a.M + 3) / 4, parts), dim3(64), 0, st, a);
-    } else {
-        hipLaunchKernelGGL(request_tile_kernel, dim3((unsigned)(a.M + 15) / 16, (unsigned)a.r / 16), dim3(64 * kTileWaves), 0, st, a);
+    if (a.M <= 512) {
+        hipLaunchKernelGGL(request_rows_kernel, dim3((unsigned)a.M, (unsigned)a.r / kDownColumns), dim3(64), 0, st, a);
+        return hipGetLastError();
     }
+    const RequestTileArgs t{a, (a.M + 15) / 16, a.r / 16};
+    const int64_t by_rows = ((int64_t)a.M * 4 * t.parts + kTileWaves - 1) / kTileWaves;
+    hipLaunchKernelGGL(request_tile_kernel, dim3((unsigned)((int64_t)t.tiles * t.parts + by_rows)), dim3(64 * kTileWaves), 0, st, t);
     return hipGetLastError();
 }
 

@@ -81,7 +81,7 @@ lora_status lora_requests_fwd(const lora_bf16* X, const lora_bf16* W, const lora
                               const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P, lora_bf16* Y,
                               lora_bf16* S, lora_stream stream) {
     if (M < 0 || K <= 0 || N <= 0 || M >= (1ll << 31) || K >= (1ll << 31) || N >= (1ll << 31) || P < 1 || P >= (1ll << 31)) return LORA_ERR_SHAPE;
-    if ((K & 63) || (N & 63) || K > (1 << 22) || N > (1 << 22) || !(r == 16 || r == 32 || r == 64)) return LORA_ERR_UNSUPPORTED;
+    if ((K & 63) || (N & 63) || K > (1 << 22) || N > (1 << 22) || !(r == 16 || r == 32 || r == 64) || M >= (1 << 21)) return LORA_ERR_UNSUPPORTED;
     if (!W || !A || !B || !s || (M > 0 && (!X || !ids || !Y || !S))) return LORA_ERR_NULL;
     if (misaligned(X) || misaligned(W) || misaligned(A) || misaligned(B) || misaligned(Y) || misaligned(S)) return LORA_ERR_ALIGN;
     if (misaligned(ids, 4) || misaligned(ranks, 4) || misaligned(s, 4)) return LORA_ERR_ALIGN;

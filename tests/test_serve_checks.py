@@ -29,7 +29,7 @@ def test_requests(lib):
     for name in ("X", "W", "A", "B", "ids", "s", "Y", "S"):
         assert f(**{name: None}) == NULL, name
     assert [f(M=-1), f(K=0), f(N=-64), f(P=0), f(M=1 << 31)] == [SHAPE] * 5
-    assert [f(K=96), f(N=100), f(r=8), f(r=48), f(K=1 << 23)] == [UNSUPPORTED] * 5
+    assert [f(K=96), f(N=100), f(r=8), f(r=48), f(K=1 << 23), f(M=1 << 21)] == [UNSUPPORTED] * 6
     for name in ("X", "W", "A", "B", "Y", "S"):
         assert f(**{name: P(0x1008)}) == ALIGN, name
     assert f(ids=P(0x1002)) == ALIGN and f(ranks=P(0x1001)) == ALIGN and f(s=P(0x1002)) == ALIGN
