@@ -368,19 +368,23 @@ def ceiling_hbm_read(src, sink, workgroups) -> int:
 
 
 # ---- serving adapters, and what stands behind the query and key projections -----------------------------
-def _typed(dtype, *tensors):
-    for t in tensors:
-        if t is not None:
-            assert t.is_cuda and t.dtype == dtype, f"a GPU tensor of {dtype} is wanted, not {t.dtype} on {t.device}"
+# (a decode step's launches run for 3 - 5 us each: the checks look at every tensor once, and pointers go as numbers)
+_BF16, _F32, _I32, _FP8 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+
+
+def _at(t: torch.Tensor, dtype) -> int:
+    """Pointer of a contiguous GPU tensor of this type."""
+    assert t.dtype is dtype and t.is_cuda and t.is_contiguous(), f"a contiguous GPU tensor of {dtype} is wanted, not {t.dtype} on {t.device}"
+    return t.data_ptr()
 
 
 def _heads(t: torch.Tensor):
     """Pointer and row stride of [rows, heads, dim] whose rows may be apart (a part of a fused projection's output)."""
-    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3, "bfloat16 [rows, heads, dim] on the GPU is wanted"
     n, h, d = t.shape
     s = t.stride()
-    assert (d == 1 or s[2] == 1) and (h == 1 or s[1] == d), "the heads of a row must lie side by side"
-    return t.data_ptr(), (s[0] if n > 1 else h * d)
+    assert t.dtype is _BF16 and t.is_cuda, f"bfloat16 [rows, heads, dim] on the GPU is wanted, not {t.dtype} on {t.device}"
+    assert (s[2] == 1 or d == 1) and (s[1] == d or h == 1), "the heads of a row must lie side by side"
+    return t.data_ptr(), s[0] if n > 1 else h * d
 
 
 def lora_requests_fwd(X, W, A, B, ids, s, ranks=None, Y=None, S=None):
@@ -388,40 +392,37 @@ def lora_requests_fwd(X, W, A, B, ids, s, ranks=None, Y=None, S=None):
     bf16; ids [M] int32, s [P] fp32 and ranks [P] int32 (optional) on the GPU."""
     M, K = X.shape
     P, N, r = B.shape
-    assert tuple(W.shape) == (N, K) and tuple(A.shape) == (P, r, K) and ids.numel() == M and s.numel() == P, "shapes do not fit"
-    _typed(torch.bfloat16, X, W, A, B, Y, S)
-    _typed(torch.int32, ids, ranks)
-    _typed(torch.float32, s)
-    assert ranks is None or ranks.numel() == P, "a rank for every adapter"
-    Y = torch.empty((M, N), dtype=torch.bfloat16, device=X.device) if Y is None else Y
-    S = torch.empty((M, r), dtype=torch.bfloat16, device=X.device) if S is None else S
-    assert tuple(Y.shape) == (M, N) and tuple(S.shape) == (M, r), "shapes do not fit"
-    _check(load_library().lora_requests_fwd(_ptr(X), _ptr(W), _ptr(A), _ptr(B), _ptr(ids), _ptr(ranks), _ptr(s), M, K, N, r, P, _ptr(Y),
-                                            _ptr(S), _stream()))
+    Y = torch.empty((M, N), dtype=_BF16, device=X.device) if Y is None else Y
+    S = torch.empty((M, r), dtype=_BF16, device=X.device) if S is None else S
+    assert W.shape == (N, K) and A.shape == (P, r, K) and ids.numel() == M and s.numel() == P and (ranks is None or ranks.numel() == P) and \
+        Y.shape == (M, N) and S.shape == (M, r), "shapes do not fit"
+    _check(load_library().lora_requests_fwd(_at(X, _BF16), _at(W, _BF16), _at(A, _BF16), _at(B, _BF16), _at(ids, _I32),
+                                            None if ranks is None else _at(ranks, _I32), _at(s, _F32), M, K, N, r, P, _at(Y, _BF16),
+                                            _at(S, _BF16), _stream()))
     return Y, S
 
 
-def _rope_args(q, k, gq, gk, cos, sin, pos):
+def _rope_sizes(q, k, gq, gk, cos, sin, pos):
     M, H, D = q.shape
     G = k.shape[1]
-    assert tuple(k.shape) == (M, G, D) and gq.numel() == D and gk.numel() == D and pos.numel() == M and cos.shape == sin.shape and cos.dim() == 2, \
-        "shapes do not fit"
-    _typed(torch.bfloat16, gq, gk)
-    _typed(torch.float32, cos, sin)
-    _typed(torch.int32, pos)
-    return M, H, G, D, 2 * cos.shape[1], cos.shape[0]
+    positions, half = cos.shape
+    assert k.shape == (M, G, D) and gq.numel() == D and gk.numel() == D and pos.numel() == M and cos.shape == sin.shape, "shapes do not fit"
+    return M, H, G, D, 2 * half, positions
 
 
 def lora_qk_norm_rope_fwd(q, k, gq, gk, cos, sin, pos, eps=1e-6, interleaved=False, q_out=None, k_out=None):
     """q_out [M,H,D], k_out [M,G,D]: RMS norm of every head of q [M,H,D] and k [M,G,D] (rows may be apart) with gq, gk [D], turned by row
     pos[i] (int32) of cos, sin [positions, rot/2] fp32."""
-    M, H, G, D, rot, positions = _rope_args(q, k, gq, gk, cos, sin, pos)
-    q_out = torch.empty((M, H, D), dtype=torch.bfloat16, device=q.device) if q_out is None else q_out
-    k_out = torch.empty((M, G, D), dtype=torch.bfloat16, device=q.device) if k_out is None else k_out
+    M, H, G, D, rot, positions = _rope_sizes(q, k, gq, gk, cos, sin, pos)
+    q_out = torch.empty((M, H, D), dtype=_BF16, device=q.device) if q_out is None else q_out
+    k_out = torch.empty((M, G, D), dtype=_BF16, device=q.device) if k_out is None else k_out
     assert q_out.shape == q.shape and k_out.shape == k.shape, "shapes do not fit"
-    (qp, ldq), (kp, ldk), (qo, ldqo), (ko, ldko) = _heads(q), _heads(k), _heads(q_out), _heads(k_out)
-    _check(load_library().lora_qk_norm_rope_fwd(qp, kp, _ptr(gq), _ptr(gk), _ptr(cos), _ptr(sin), _ptr(pos), M, H, G, D, rot, positions, ldq,
-                                                ldk, ldqo, ldko, eps, int(interleaved), qo, ko, _stream()))
+    qp, ldq = _heads(q)
+    kp, ldk = _heads(k)
+    qo, ldqo = _heads(q_out)
+    ko, ldko = _heads(k_out)
+    _check(load_library().lora_qk_norm_rope_fwd(qp, kp, _at(gq, _BF16), _at(gk, _BF16), _at(cos, _F32), _at(sin, _F32), _at(pos, _I32), M, H, G, D,
+                                                rot, positions, ldq, ldk, ldqo, ldko, eps, interleaved, qo, ko, _stream()))
     return q_out, k_out
 
 
@@ -432,62 +433,64 @@ def alloc_qk_norm_rope_workspace(M, H, G, D, device="cuda") -> torch.Tensor:
 def lora_qk_norm_rope_bwd(q, k, gq, gk, cos, sin, pos, dq_out, dk_out, eps=1e-6, interleaved=False, dq=None, dk=None, dgq=None, dgk=None,
                           accumulate=False, workspace=None):
     """dq, dk (bf16, as q and k), dgq, dgk [D] fp32 of lora_qk_norm_rope_fwd for the gradients dq_out, dk_out of its outputs."""
-    M, H, G, D, rot, positions = _rope_args(q, k, gq, gk, cos, sin, pos)
-    dq = torch.empty((M, H, D), dtype=torch.bfloat16, device=q.device) if dq is None else dq
-    dk = torch.empty((M, G, D), dtype=torch.bfloat16, device=q.device) if dk is None else dk
-    dgq = torch.empty(D, dtype=torch.float32, device=q.device) if dgq is None else dgq
-    dgk = torch.empty(D, dtype=torch.float32, device=q.device) if dgk is None else dgk
+    M, H, G, D, rot, positions = _rope_sizes(q, k, gq, gk, cos, sin, pos)
+    dq = torch.empty((M, H, D), dtype=_BF16, device=q.device) if dq is None else dq
+    dk = torch.empty((M, G, D), dtype=_BF16, device=q.device) if dk is None else dk
+    dgq = torch.empty(D, dtype=_F32, device=q.device) if dgq is None else dgq
+    dgk = torch.empty(D, dtype=_F32, device=q.device) if dgk is None else dgk
     assert dq.shape == q.shape == dq_out.shape and dk.shape == k.shape == dk_out.shape and dgq.numel() == D and dgk.numel() == D, "shapes do not fit"
-    _typed(torch.float32, dgq, dgk)
     ws = alloc_qk_norm_rope_workspace(M, H, G, D, q.device) if workspace is None else workspace
     (qp, ldq), (kp, ldk), (qo, ldqo), (ko, ldko), (dqp, lddq), (dkp, lddk) = (_heads(t) for t in (q, k, dq_out, dk_out, dq, dk))
-    _check(load_library().lora_qk_norm_rope_bwd(qp, kp, _ptr(gq), _ptr(gk), _ptr(cos), _ptr(sin), _ptr(pos), qo, ko, M, H, G, D, rot, positions,
-                                                ldq, ldk, ldqo, ldko, lddq, lddk, eps, int(interleaved), dqp, dkp, _ptr(dgq), _ptr(dgk),
-                                                int(accumulate), _ptr(ws), ws.numel(), _stream()))
+    _check(load_library().lora_qk_norm_rope_bwd(qp, kp, _at(gq, _BF16), _at(gk, _BF16), _at(cos, _F32), _at(sin, _F32), _at(pos, _I32), qo, ko, M, H, G,
+                                                D, rot, positions, ldq, ldk, ldqo, ldko, lddq, lddk, eps, interleaved, dqp, dkp, _at(dgq, _F32),
+                                                _at(dgk, _F32), accumulate, _at(ws, torch.uint8), ws.numel(), _stream()))
     return dq, dk, dgq, dgk
 
 
 class KVCache:
     """A paged cache over tensors that the caller holds: k, v [pages, heads, page, dim], bf16, or fp8 (torch.float8_e4m3fn) with
     the biased exponents k_exp, v_exp [pages, heads, page] (uint8) of a power of two for every token and head."""
+    __slots__ = ("tensors", "pages", "heads", "page", "dim", "_c", "_ref")
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
-        fp8 = k.dtype == torch.float8_e4m3fn
-        assert k.dim() == 4 and k.shape == v.shape, "k and v are [pages, heads, page, dim]"
-        _typed(torch.float8_e4m3fn if fp8 else torch.bfloat16, k, v)
-        assert not fp8 or (k_exp is not None and v_exp is not None and k_exp.shape == v_exp.shape == k.shape[:3]), "an exponent for every token and head"
-        if fp8:
-            _typed(torch.uint8, k_exp, v_exp)
-        self.tensors = (k, v, k_exp, v_exp) if fp8 else (k, v, None, None)
-        self.pages, self.heads, self.page, self.dim = k.shape
-        self._c = CacheArrays(*(_ptr(t) for t in self.tensors), self.pages, self.page, self.heads, self.dim, int(fp8))
+        shape = k.shape
+        assert len(shape) == 4 and v.shape == shape, "k and v are [pages, heads, page, dim]"
+        self.pages, self.heads, self.page, self.dim = shape
+        if k.dtype is _FP8:
+            assert k_exp is not None and v_exp is not None and k_exp.shape == v_exp.shape == shape[:3], "an exponent for every token and head"
+            self.tensors = (k, v, k_exp, v_exp)
+            self._c = CacheArrays(_at(k, _FP8), _at(v, _FP8), _at(k_exp, torch.uint8), _at(v_exp, torch.uint8), shape[0], shape[2], shape[1], shape[3],
+                                  1)
+        else:
+            self.tensors = (k, v, None, None)
+            self._c = CacheArrays(_at(k, _BF16), _at(v, _BF16), None, None, shape[0], shape[2], shape[1], shape[3], 0)
         self._ref = C.byref(self._c)
 
     @classmethod
     def empty(cls, pages, page, heads, dim, fp8=False, device="cuda"):
-        k, v = (torch.zeros((pages, heads, page, dim), dtype=torch.float8_e4m3fn if fp8 else torch.bfloat16, device=device) for _ in range(2))
+        k, v = (torch.zeros((pages, heads, page, dim), dtype=_FP8 if fp8 else _BF16, device=device) for _ in range(2))
         exps = (torch.zeros((pages, heads, page), dtype=torch.uint8, device=device) for _ in range(2)) if fp8 else (None, None)
         return cls(k, v, *exps)
 
 
 def lora_kv_cache_write(cache: KVCache, k, v, slots):
     """Rows of k, v [M, heads, dim] (rows may be apart) to the slots (int64: page number * page + place; outside the cache: left out)."""
-    M = k.shape[0]
-    assert tuple(k.shape) == tuple(v.shape) == (M, cache.heads, cache.dim) and slots.numel() == M, "shapes do not fit"
-    _typed(torch.int64, slots)
-    (kp, ldk), (vp, ldv) = _heads(k), _heads(v)
-    _check(load_library().lora_kv_cache_write(cache._ref, kp, vp, ldk, ldv, _ptr(slots), M, _stream()))
+    M = slots.numel()
+    assert k.shape == (M, cache.heads, cache.dim) and v.shape == k.shape, "shapes do not fit"
+    kp, ldk = _heads(k)
+    vp, ldv = _heads(v)
+    _check(load_library().lora_kv_cache_write(cache._ref, kp, vp, ldk, ldv, _at(slots, torch.int64), M, _stream()))
 
 
 def lora_kv_cache_read(cache: KVCache, slots, k=None, v=None):
     """k, v [M, heads, dim] bf16 of the slots (outside the cache: zeros)."""
     M = slots.numel()
-    _typed(torch.int64, slots)
-    k = torch.empty((M, cache.heads, cache.dim), dtype=torch.bfloat16, device=slots.device) if k is None else k
-    v = torch.empty((M, cache.heads, cache.dim), dtype=torch.bfloat16, device=slots.device) if v is None else v
-    assert tuple(k.shape) == tuple(v.shape) == (M, cache.heads, cache.dim), "shapes do not fit"
-    (kp, ldk), (vp, ldv) = _heads(k), _heads(v)
-    _check(load_library().lora_kv_cache_read(cache._ref, _ptr(slots), M, kp, vp, ldk, ldv, _stream()))
+    k = torch.empty((M, cache.heads, cache.dim), dtype=_BF16, device=slots.device) if k is None else k
+    v = torch.empty((M, cache.heads, cache.dim), dtype=_BF16, device=slots.device) if v is None else v
+    assert k.shape == (M, cache.heads, cache.dim) and v.shape == k.shape, "shapes do not fit"
+    kp, ldk = _heads(k)
+    vp, ldv = _heads(v)
+    _check(load_library().lora_kv_cache_read(cache._ref, _at(slots, torch.int64), M, kp, vp, ldk, ldv, _stream()))
     return k, v
 
 
@@ -501,14 +504,14 @@ def lora_paged_attn_fwd(q, cache: KVCache, table, offsets, kv_lens, max_new, max
     cache holds of each in the pages table[b] (int32 [sequences, pages], as offsets and kv_lens), the new ones among them."""
     T, H, D = q.shape
     B, max_pages = table.shape
-    assert D == cache.dim and offsets.numel() == B + 1 and kv_lens.numel() == B, "shapes do not fit"
-    _typed(torch.int32, table, offsets, kv_lens)
-    assert max_pages <= 1 or table.stride(1) == 1, "the pages of a sequence must lie side by side"
-    out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device) if out is None else out
-    assert out.shape == q.shape, "shapes do not fit"
+    out = torch.empty((T, H, D), dtype=_BF16, device=q.device) if out is None else out
+    assert D == cache.dim and offsets.numel() == B + 1 and kv_lens.numel() == B and out.shape == q.shape, "shapes do not fit"
+    ldt, one = table.stride()
+    assert table.dtype is _I32 and table.is_cuda and (one == 1 or max_pages <= 1), "int32 pages on the GPU, those of a sequence side by side, are wanted"
     ws = alloc_paged_attn_workspace(cache, T, H, B, max_new, max_kv, window, q.device) if workspace is None else workspace
-    (qp, ldq), (op, ldo) = _heads(q), _heads(out)
-    _check(load_library().lora_paged_attn_fwd(qp, cache._ref, table.data_ptr(), _ptr(offsets), _ptr(kv_lens), T, H, B, max_pages, ldq,
-                                              table.stride(0) if B > 1 else max_pages, ldo, max_new, max_kv, D ** -0.5 if scale is None else scale,
-                                              window, op, _ptr(ws), ws.numel(), _stream()))
+    qp, ldq = _heads(q)
+    op, ldo = _heads(out)
+    _check(load_library().lora_paged_attn_fwd(qp, cache._ref, table.data_ptr(), _at(offsets, _I32), _at(kv_lens, _I32), T, H, B, max_pages, ldq,
+                                              ldt if B > 1 else max_pages, ldo, max_new, max_kv, D ** -0.5 if scale is None else scale, window, op,
+                                              _at(ws, torch.uint8), ws.numel(), _stream()))
     return out
