@@ -5,12 +5,17 @@
 // fp32, the result is rounded once.  Bound by HBM: 4 (6) bytes an element.  Eight entries to a lane (16-byte loads), 8, 16 or
 // 32 lanes to a head by its size; a head's sums are butterflies over its lanes.  With R's cosines and sines multiplied by gamma once per
 // row, y is one product and one multiply-add an entry; a pair's other entry comes from the lane that holds it, as the bf16 it was.
+#include <algorithm>
+
 #include "lf_serve.h"
 
 namespace lf {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeBlocks = 4 * kComputeUnits;      // of the backward: each leaves a plane of partial sums, so no more than fill the chip
+// The backward: each workgroup leaves a plane of partial sums, so no more than the registers let run at once, four on every compute unit, of four waves, or
+// (32 lanes to a head) three.  us, of 4 / 8 / 16 waves: 5003 rows of 64 + 8 heads 60.9 / 63.6 / 65.5, 16000 rows of 32 + 8 100 / 105 / 105.
+constexpr int kRopeBlocks = 4 * kComputeUnits;
+constexpr int rope_bwd_waves(int lanes) { return lanes == 32 ? 3 : 4; }
 
 // GL lanes to a head, a wave for a row, or for a part of its heads.
 template <int GL, bool INTER>
@@ -72,10 +77,10 @@ __device__ __forceinline__ void others(const RopeLane<GL, INTER>& ln, u32x4 raw,
 }
 
 template <int GL, bool INTER>
-__device__ __forceinline__ void gamma_of(const lora_bf16* g, const RopeLane<GL, INTER>& ln, float (&own)[8]) {
+__device__ __forceinline__ u32x4 gamma_of(const lora_bf16* g, const RopeLane<GL, INTER>& ln) {
     u32x4 v = u32x4{0u, 0u, 0u, 0u};
     if (ln.active) v = *(const u32x4*)(g + 8 * ln.j);
-    unpack8(v, own);
+    return v;
 }
 
 // A wave's row is done in passes of 64 / GL heads, first the queries' passes, then the keys'; part i of the row takes passes i, i + parts, ..
@@ -102,8 +107,9 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
         float c[8], s[8], g[8], o[8];
         angles(p, ln, pos, known, c, s);
         auto fold = [&](const lora_bf16* gamma, float (&cg)[8], float (&sg)[8]) {
-            gamma_of(gamma, ln, g);
-            others(ln, pack8(g), o);                       // (gamma is bf16: packing it again is exact)
+            const u32x4 raw = gamma_of(gamma, ln);
+            unpack8(raw, g);
+            others(ln, raw, o);
 #pragma unroll
             for (int i = 0; i < 8; ++i) { cg[i] = c[i] * g[i]; sg[i] = s[i] * o[i]; }
         };
@@ -146,25 +152,27 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
 }
 
 template <int GL, bool INTER>
-__global__ void __launch_bounds__(kRopeThreads, GL == 32 ? 3 : 4) rope_bwd_kernel(RopeArgs p) {
-    __shared__ float red[kRopeThreads / 64][2][GL * 8];
+__global__ void __launch_bounds__(64 * rope_bwd_waves(GL), rope_bwd_waves(GL)) rope_bwd_kernel(RopeArgs p) {
+    constexpr int WAVES = rope_bwd_waves(GL);
+    __shared__ float red[WAVES][2][GL * 8];
     const RopeLane<GL, INTER> ln(p.D, p.rot);
     const RopePasses<GL> ps(p.H, p.G);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    float gq[8], gk[8], dgq[8], dgk[8];
-    gamma_of(p.gamma_q, ln, gq);
-    gamma_of(p.gamma_k, ln, gk);
+    float dgq[8], dgk[8];
+    const u32x4 gq = gamma_of(p.gamma_q, ln), gk = gamma_of(p.gamma_k, ln);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dgq[i] = dgk[i] = 0.f;
     const int64_t units = p.M * p.parts;
-    for (int64_t unit = (int64_t)blockIdx.x * (kRopeThreads / 64) + w; unit < units; unit += (int64_t)gridDim.x * (kRopeThreads / 64)) {
+    for (int64_t unit = (int64_t)blockIdx.x * WAVES + w; unit < units; unit += (int64_t)gridDim.x * WAVES) {
         const int64_t row = unit / p.parts;
         const int pos = p.pos[row];
         const bool known = pos >= 0 && pos < p.positions;
         float c[8], s[8];
         angles(p, ln, pos, known, c, s);
-        auto heads = [&](const lora_bf16* x_row, const lora_bf16* dy_row, lora_bf16* out_row, int n, int passes, int first, const float (&g)[8],
+        auto heads = [&](const lora_bf16* x_row, const lora_bf16* dy_row, lora_bf16* out_row, int n, int passes, int first, u32x4 gamma,
                          float (&dg)[8]) {
+            float g[8];
+            unpack8(gamma, g);
             constexpr int U = 2;
             for (; first < passes; first += U * p.parts) {
                 u32x4 xr[U], dr[U];
@@ -226,44 +234,45 @@ __global__ void __launch_bounds__(kRopeThreads, GL == 32 ? 3 : 4) rope_bwd_kerne
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * p.D; i += kRopeThreads) {
+    for (int i = threadIdx.x; i < 2 * p.D; i += 64 * WAVES) {
         const int t = i >= p.D, d = i - t * p.D;
-        p.part[(int64_t)blockIdx.x * 2 * p.D + i] = ((red[0][t][d] + red[1][t][d]) + red[2][t][d]) + red[3][t][d];
+        float sum = red[0][t][d];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v) sum += red[v][t][d];
+        p.part[(int64_t)blockIdx.x * 2 * p.D + i] = sum;
     }
 }
 
-// dgamma (+)= the sum over the blocks' planes: eight columns to a workgroup, two threads to a plane, each of them with every 128th.  All loads of
-// a thread are under way together: with 16 workgroups of 16 columns, whose threads went through 64 planes one by one, 1024 planes took 20 us.
-__global__ void __launch_bounds__(256) rope_finalize_kernel(RopeFinalizeArgs p) {
-    __shared__ f32x4 red[128][2];
-    const int half = threadIdx.x & 1, sl = threadIdx.x >> 1, c = blockIdx.x * 8 + 4 * half;
-    f32x4 v[kRopeBlocks / 128];
+// dgamma (+)= the sum over the workgroups' planes: a wave for four columns, all loads under way together.
+__global__ void __launch_bounds__(64) rope_finalize_kernel(RopeFinalizeArgs p) {
+    const int l = threadIdx.x, c = blockIdx.x * 4;
+    f32x4 v[kRopeBlocks / 64];
 #pragma unroll
-    for (int i = 0; i < kRopeBlocks / 128; ++i) {
+    for (int i = 0; i < kRopeBlocks / 64; ++i) {
         v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (sl + 128 * i < p.blocks) v[i] = *(const f32x4*)(p.part + (int64_t)(sl + 128 * i) * 2 * p.D + c);
+        if (l + 64 * i < p.blocks) v[i] = *(const f32x4*)(p.part + (int64_t)(l + 64 * i) * 2 * p.D + c);
     }
 #pragma unroll
-    for (int i = 1; i < kRopeBlocks / 128; ++i) v[0] += v[i];
-    red[sl][half] = v[0];
+    for (int i = 1; i < kRopeBlocks / 64; ++i) v[0] += v[i];
 #pragma unroll
-    for (int n = 64; n > 0; n >>= 1) {
-        __syncthreads();
-        if (sl < n) red[sl][half] += red[sl + n][half];
-    }
-    if (sl) return;
-    v[0] = red[0][half];
+    for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[0][e] += __shfl_xor(v[0][e], o);
+    if (l) return;
     float* out = c < p.D ? p.dgamma_q + c : p.dgamma_k + c - p.D;
     if (p.accumulate) v[0] += *(const f32x4*)out;
     *(f32x4*)out = v[0];
 }
 
-// Parts of a row while there are fewer rows than 16 waves to a compute unit, but no more than its passes.
+// Parts of a row: more than one while there are fewer rows than 16 waves to a compute unit.  Backward, whose waves go on to further rows: about
+// four passes to a part, so that the waves end together, and an odd number, so that a wave doesn't meet the same part in every row. us, parts 1 / 2 /
+// 3 / 4 / 5 / 6: 5003 rows of 64 + 8 heads (18 passes) 70.6 / 64.5 / 63.9 / 65.3 / 62.3 / 62.0; 8192 rows of 32 + 8 (10) 61.8 / 60.1 / 59.4 / 61.9 / 59.4 / 61.1;
+// 5003 of 8 + 2, D = 256 (5) 26.0 / 29.9 / 30.4 / 39.5.  (Forward, 8192 rows of 32 + 8: 39.3 / 45.5, each part forms the row's factors anew.)
 template <int GL>
-static int rope_parts(int64_t M, int H, int G) {
+static int rope_parts(int64_t M, int H, int G, bool backward) {
     const int all = RopePasses<GL>(H, G).all;
-    const int64_t want = (16 * kComputeUnits + M - 1) / (M > 0 ? M : 1);
-    return (int)(want < all ? want : all);
+    const int64_t want = std::max((16 * kComputeUnits + M - 1) / std::max<int64_t>(M, 1), (int64_t)(backward ? (all + 2) / 4 | 1 : 1));
+    return (int)std::min<int64_t>(want, all);
 }
 template <class F>
 static auto with_lanes(int D, F&& f) {
@@ -274,7 +283,7 @@ static auto with_lanes(int D, F&& f) {
 
 hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st) {
     return with_lanes(a.D, [&](auto gl) {
-        a.parts = rope_parts<gl()>(a.M, a.H, a.G);
+        a.parts = rope_parts<gl()>(a.M, a.H, a.G, false);
         const int64_t blocks = (a.M * a.parts + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
         if (interleaved) hipLaunchKernelGGL((rope_fwd_kernel<gl(), true>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
         else hipLaunchKernelGGL((rope_fwd_kernel<gl(), false>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
@@ -284,7 +293,7 @@ hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st) {
 
 int rope_blocks(int64_t M, int H, int G, int D) {
     return with_lanes(D, [&](auto gl) {
-        const int64_t n = (M * rope_parts<gl()>(M, H, G) + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
+        const int64_t n = (M * rope_parts<gl()>(M, H, G, true) + rope_bwd_waves(gl()) - 1) / rope_bwd_waves(gl());
         return (int)(n < kRopeBlocks ? n : kRopeBlocks);
     });
 }
@@ -292,14 +301,14 @@ int rope_blocks(int64_t M, int H, int G, int D) {
 hipError_t launch_rope_bwd(RopeArgs a, bool interleaved, const RopeFinalizeArgs& f, hipStream_t st) {
     if (f.blocks > 0) {
         const hipError_t e = with_lanes(a.D, [&](auto gl) {
-            a.parts = rope_parts<gl()>(a.M, a.H, a.G);
-            if (interleaved) hipLaunchKernelGGL((rope_bwd_kernel<gl(), true>), dim3(f.blocks), dim3(kRopeThreads), 0, st, a);
-            else hipLaunchKernelGGL((rope_bwd_kernel<gl(), false>), dim3(f.blocks), dim3(kRopeThreads), 0, st, a);
+            a.parts = rope_parts<gl()>(a.M, a.H, a.G, true);
+            if (interleaved) hipLaunchKernelGGL((rope_bwd_kernel<gl(), true>), dim3(f.blocks), dim3(64 * rope_bwd_waves(gl())), 0, st, a);
+            else hipLaunchKernelGGL((rope_bwd_kernel<gl(), false>), dim3(f.blocks), dim3(64 * rope_bwd_waves(gl())), 0, st, a);
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(rope_finalize_kernel, dim3(2 * a.D / 8), dim3(256), 0, st, f);
+    hipLaunchKernelGGL(rope_finalize_kernel, dim3(2 * a.D / 4), dim3(64), 0, st, f);
     return hipGetLastError();
 }
 
