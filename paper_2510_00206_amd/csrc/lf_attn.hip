@@ -56,7 +56,8 @@ __device__ __forceinline__ bool attn_tile(const AttnArgs& p, AttnTile& t) {
     // Key/value heads of a sequence fastest: with eight heads the tiles that share keys are on one XCD.  Then tiles, the last first, since they see the
     // most keys; parts slowest: the last ones, which hold what is left of a range, run last.  Within an XCD workgroups go to its four
     // shader engines in turn, full or not: with sequences before tiles, two of them (5003 and 16000 keys, 1021 new tokens) left half
-    // the engines without work for half of the time (515 us instead of 363).
+    // the engines without work for half of the time (515 us instead of 363).  Every part starts at another sequence, so that the parts of a long
+    // one are not all on the same compute units (this launch and the join, us: 300 -> 275; four sequences of 33000 - 131072, few rows: 260 -> 254).
     int id = blockIdx.x;
     t.g = id % p.c.heads;
     id /= p.c.heads;
@@ -64,6 +65,7 @@ __device__ __forceinline__ bool attn_tile(const AttnArgs& p, AttnTile& t) {
     id /= p.tiles;
     t.b = id % p.B;
     t.split = id / p.B;
+    t.b = (t.b + t.split * (p.B / 4 + 1)) % p.B;
     if (!attn_rows<BM>(p, t) || t.split >= t.parts) return false;
     t.k0 = t.key_lo + t.split * p.split_keys;
     t.k1 = t.split + 1 == p.splits ? t.key_hi : min(t.key_hi, t.k0 + p.split_keys);     // (the last takes what there is: lengths past max_kv)
@@ -249,7 +251,7 @@ __device__ __forceinline__ const lora_bf16* q_row(const AttnArgs& p, const AttnT
 // Four entries from `d` on of a finished row: o = sum of p v, l = sum of p, m = their reference.
 __device__ __forceinline__ void put(const AttnArgs& p, const AttnTile& t, int row, int d, f32x4 o, float m, float l) {
     const int tok = row / p.group, head = t.g * p.group + row - tok * p.group;
-    if (p.splits > 1) {
+    if (t.parts > 1) {
         const int64_t at = (int64_t)t.split * p.T * p.H + (int64_t)(t.first + tok) * p.H + head;
         *(f32x4*)(p.part_o + at * p.c.D + d) = o;
         if (d == 0) {
@@ -832,51 +834,81 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
 }
 
 // ---- the parts' results, joined ---------------------------------------------------------------------
-// A wave for a row, D / 64 entries to a lane; lane i holds the maximum and sum of parts i, i + 64, .., and the rows of eight parts are under way together.
+// D / 4 lanes read a row of a part, four entries each; running maximum and sum as in the kernels, four parts a step.  Many rows: each of these groups of lanes
+// (8 of a workgroup, D = 64: 16) has a row of its own and goes through its parts.  Few rows, of perhaps many parts: a workgroup for a row, the parts shared
+// out over the groups, whose results are joined in a fixed order.
 template <int D, int BM>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs p) {
-    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int LANES = D / 4, SLOTS = 256 / LANES, U = 4;
+    constexpr bool SPREAD = BM < 128;
+    constexpr int STEP = SPREAD ? SLOTS : 1;
+    const int slot = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
     AttnTile t;
-    const int per = (p.tiles * BM + 3) / 4;                 // workgroups for a head of a sequence
+    const int per = (int)gridDim.x / (p.c.heads * p.B);     // workgroups for a head of a sequence
     int id = blockIdx.x;
-    const int row = id % per * 4 + w;
+    const int row0 = id % per * (SPREAD ? 1 : SLOTS), row = SPREAD ? row0 : row0 + slot;
     id /= per;
     t.g = id % p.c.heads;
     t.b = id / p.c.heads;
-    t.tile = row / BM;
-    if (!attn_rows<BM>(p, t) || row - t.row0 >= t.rows) return;
+    t.tile = row0 / BM;
+    if (!attn_rows<BM>(p, t) || t.parts == 1 || row - t.row0 >= t.rows) return;
     const int tok = row / p.group, head = t.g * p.group + row - tok * p.group;
     const int64_t at = (int64_t)(t.first + tok) * p.H + head, plane = (int64_t)p.T * p.H;
-    float m = kNone;
-    for (int i = l; i < t.parts; i += 64) m = fmaxf(m, p.part_ml[2 * (i * plane + at)]);
+    float m = kNone, sum = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i0 = SPREAD ? slot : 0; i0 < t.parts; i0 += U * STEP) {
+        f32x4 v[U];
+        float pm[U], pl[U];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    constexpr int E = D / 64, U = 8;
-    typedef __attribute__((ext_vector_type(E))) float row_t;
-    float sum = 0.f;
-    row_t o = {};
-    for (int i0 = 0; i0 < t.parts; i0 += 64) {
-        float f = 0.f;                                      // of part i0 + l
-        if (i0 + l < t.parts) {
-            const float* ml = p.part_ml + 2 * ((i0 + l) * plane + at);
-            f = __builtin_amdgcn_exp2f(ml[0] - m);
-            sum += f * ml[1];
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * STEP;
+            pm[u] = kNone;
+            pl[u] = 0.f;
+            v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (i < t.parts) {
+                const float* ml = p.part_ml + 2 * (i * plane + at);
+                pm[u] = ml[0];
+                pl[u] = ml[1];
+                v[u] = *(const f32x4*)(p.part_o + (i * plane + at) * D + d);
+            }
         }
-        for (int i = i0; i < min(i0 + 64, t.parts); i += U) {
-            row_t v[U];
+        float top = m;
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = *(const row_t*)(p.part_o + (min(i + u, t.parts - 1) * plane + at) * D + E * l);
+        for (int u = 0; u < U; ++u) top = fmaxf(top, pm[u]);
+        const float back = __builtin_amdgcn_exp2f(m - top);
+        o *= back;
+        sum *= back;
+        m = top;
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u < t.parts) o += v[u] * __shfl(f, (i + u) & 63);
+        for (int u = 0; u < U; ++u) {
+            const float f = __builtin_amdgcn_exp2f(pm[u] - top);
+            o += v[u] * f;
+            sum += pl[u] * f;
         }
     }
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
+    if constexpr (SPREAD) {
+        __shared__ f32x4 red_o[SLOTS][LANES];
+        __shared__ float red_ml[SLOTS][2];
+        red_o[slot][d / 4] = o;
+        if (d == 0) {
+            red_ml[slot][0] = m;
+            red_ml[slot][1] = sum;
+        }
+        __syncthreads();
+        if (slot) return;
+        const int n = min(SLOTS, t.parts);
+        for (int i = 1; i < n; ++i) m = fmaxf(m, red_ml[i][0]);
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
+        sum = 0.f;
+        for (int i = 0; i < n; ++i) {
+            const float f = __builtin_amdgcn_exp2f(red_ml[i][0] - m);
+            o += red_o[i][d / 4] * f;
+            sum += red_ml[i][1] * f;
+        }
+    }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    lora_bf16* out = p.out + (int64_t)(t.first + tok) * p.ldo + (int64_t)head * D + E * l;
-    if constexpr (E == 1) out[0] = (lora_bf16)(pack_bf16x2(o[0] * inv, 0.f) & 0xFFFFu);
-    else *(uint32_t*)out = pack_bf16x2(o[0] * inv, o[E - 1] * inv);
+    *(u32x2*)(p.out + (int64_t)(t.first + tok) * p.ldo + (int64_t)head * D + d) =
+        u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
@@ -926,8 +958,9 @@ static hipError_t launch_attn_t(const AttnArgs& a, int rows, unsigned blocks, hi
 }
 
 template <int D>
-static hipError_t launch_join(const AttnArgs& a, int rows, hipStream_t st) {
-    const int64_t blocks = (int64_t)((a.tiles * (int64_t)rows + 3) / 4) * a.c.heads * a.B;
+static hipError_t launch_join(const AttnArgs& a, int rows, int max_new, hipStream_t st) {
+    const int64_t all = (int64_t)max_new * a.group, slots = rows < 128 ? 1 : 1024 / D;
+    const int64_t blocks = (all + slots - 1) / slots * a.c.heads * a.B;
     if (rows == 16) hipLaunchKernelGGL((attn_join_kernel<D, 16>), dim3((unsigned)blocks), dim3(256), 0, st, a);
     else if (rows == 32) hipLaunchKernelGGL((attn_join_kernel<D, 32>), dim3((unsigned)blocks), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((attn_join_kernel<D, 128>), dim3((unsigned)blocks), dim3(256), 0, st, a);
@@ -943,7 +976,7 @@ hipError_t launch_attn(AttnArgs a, const AttnPlan& p, int max_new, hipStream_t s
     if (a.c.D == 64) e = a.c.fp8 ? launch_attn_t<64, true>(a, p.rows, blocks, st) : launch_attn_t<64, false>(a, p.rows, blocks, st);
     else e = a.c.fp8 ? launch_attn_t<128, true>(a, p.rows, blocks, st) : launch_attn_t<128, false>(a, p.rows, blocks, st);
     if (e != hipSuccess || a.splits == 1) return e;
-    return a.c.D == 64 ? launch_join<64>(a, p.rows, st) : launch_join<128>(a, p.rows, st);
+    return a.c.D == 64 ? launch_join<64>(a, p.rows, max_new, st) : launch_join<128>(a, p.rows, max_new, st);
 }
 
 }  // namespace lf

@@ -93,6 +93,16 @@ def test_not_finite_stays_with_its_row():
         assert torch.equal(bad, want), M
 
 
+@pytest.mark.parametrize("r", [16, 32, 64])
+@pytest.mark.parametrize("M,N", [(3, 192), (40, 6144), (70, 256), (200, 8192), (600, 4096), (1100, 4096)])
+def test_diverged_second_factor(M, N, r):
+    """Infinities and NaN in an adapter's B reach the columns of its own rows and nothing else: neither the other rows of a tile nor those without."""
+    X, W, A, B, ids, s, _ = _case(M, 128, N, r, 8, "any", False, M + r)
+    ids[:] = torch.arange(M) % 9 - 1
+    B[2, 5, 3], B[2, 50, r - 1], B[5, N - 1, 0], B[5, 64, r // 2] = float("inf"), float("nan"), -float("inf"), float("nan")
+    _check((X, W, A, B, ids, s, None), ("diverged", M, N, r))
+
+
 def test_equals_the_layer_of_one_adapter():
     """All rows with one adapter: the forward of the training layer without dropout, up to the order of the sums in S."""
     X, W, A, B, ids, s, _ = _case(384, 512, 256, 32, 3, "one", False, 1)
