@@ -449,6 +449,7 @@ struct RequestTerm {
 #pragma unroll
         for (int t = 0; t < DEPTH; ++t)
             if (step + t < steps) step_at<false>(acc, t);
+        ring_mfma_done<MI, NI>(acc);                          // (across the blocks that are passed over the compiler keeps no distance)
         // infinity or NaN in an adapter's B has met the zeros of the block's other rows: those are done again
         float bad = 0.f;
 #pragma unroll
@@ -471,6 +472,7 @@ struct RequestTerm {
             ask(0, unit_of(step));
             step_at<true>(acc, 0);
         }
+        ring_mfma_done<MI, NI>(acc);
 #pragma unroll 1
         for (int u = 0; u < n; ++u) {
             const u32x2 unit = list.unit[u];
