@@ -1,8 +1,9 @@
 // The LoRA linear layer for many requests at once: every row names its adapter, or none, in an array on the device.
 //     S[i] = s_g X[i] A_g^T        this file        (bf16, columns past the adapter's rank zero)
 //     Y[i] = X[i] W^T + S[i] B_g^T  lf_gemm_ring.hip (the small GEMM tiles; the second term on the accumulators: request_term)
-// The first is bound by the reading of the adapters: a wave takes four columns of the rank for one row, so that a decode step of a few rows
-// is spread over the chip, or, where many rows come as chunks of few requests, 16 rows go through MFMAs at once.
+// The first is bound by the latency of ids, ranks and adapters, one after the other, and by the reading of the adapters: a wave takes two columns of the
+// rank for one row, so that a decode step of a few rows is spread over the chip, or, where many rows come as chunks of few requests, 16 rows
+// go through MFMAs at once.  Two launches: with S formed in the tiles of the second product every column tile would form it again.
 #include "lf_gemm_parts.h"
 #include "lf_gemm_ring.h"
 #include "lf_serve.h"
@@ -30,9 +31,11 @@ __device__ __forceinline__ float sum_of_wave(float v) {
     return v;
 }
 
-constexpr int kDownColumns = 4;                    // columns of the rank to a wave
+// Columns of the rank to a wave.  us, whole layer, 4 / 2 / 1: 64 rows, K = 4096, r = 16 17.6 / 17.1 / 16.9; 32 rows, K = 14336 50.3 / 46.3 / 45.8; 200 rows, r = 64
+// 101.1 / 99.8 / 101.0; 2048 rows, 37 single ones among them, r = 32 74.0 / 72.5 / 74.9.
+constexpr int kDownColumns = 2;
 
-// Columns j0 .. j0 + 3 of one row of S, by a wave.
+// Columns j0, j0 + 1 of one row of S, by a wave.
 __device__ __forceinline__ void request_row(const RequestDownArgs& p, int row, int j0) {
     constexpr int J = kDownColumns;
     const int l = threadIdx.x & 63;
@@ -56,14 +59,14 @@ __device__ __forceinline__ void request_row(const RequestDownArgs& p, int row, i
             v[j] = j0 + j < rank ? s * v[j] : 0.f;                 // (padding of A may hold anything)
         }
     }
-    if (l == 0) *(u32x2*)(p.S + (int64_t)row * p.r + j0) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    if (l == 0) *(uint32_t*)(p.S + (int64_t)row * p.r + j0) = pack_bf16x2(v[0], v[1]);
 }
 
 __global__ void __launch_bounds__(64) request_rows_kernel(RequestDownArgs p) { request_row(p, blockIdx.x, blockIdx.y * kDownColumns); }
 
 // Many rows: the 16-row tiles of one adapter by MFMAs, 16 columns of the rank to a workgroup, every eighth 64-deep slab of the contraction to a
 // wave, four of them under way at once (a lane's two 16-byte loads of a row's slab lie side by side).  The rows of the other tiles go to
-// further workgroups of the launch, a wave for each row and four columns, which find nothing to do where the tile is of one adapter.
+// further workgroups of the launch, a wave for each row and two columns, which find nothing to do where the tile is of one adapter.
 // (One after the other in their own workgroups the adapters of such tiles, 37 requests of one token among 2048 rows, took 57 us.)
 constexpr int kTileWaves = 8;
 struct RequestTileArgs { RequestDownArgs d; int tiles, parts; };       // parts: of the rank, 16 columns each
@@ -72,9 +75,10 @@ __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestTi
     const RequestDownArgs& p = a.d;
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool by_rows = (int)blockIdx.x >= a.tiles * a.parts;
-    // by rows: 4 * parts waves to a row
+    // by rows: PER waves to a row for each part
+    constexpr int PER = 16 / kDownColumns;
     const int unit = by_rows ? ((int)blockIdx.x - a.tiles * a.parts) * kTileWaves + w : 0;
-    const int own = unit / (4 * a.parts), row0 = by_rows ? own & ~15 : (int)blockIdx.x / a.parts * 16;
+    const int own = unit / (PER * a.parts), row0 = by_rows ? own & ~15 : (int)blockIdx.x / a.parts * 16;
     if (row0 >= p.M) return;
     const int row = row0 + (l & 15);
     int id = p.ids[min(row, p.M - 1)];
@@ -82,7 +86,7 @@ __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestTi
     const int g = __builtin_amdgcn_readfirstlane(id);
     const bool one = __all(id == g);
     if (by_rows) {
-        if (!one && own < p.M) request_row(p, own, unit % (4 * a.parts) * kDownColumns);
+        if (!one && own < p.M) request_row(p, own, unit % (PER * a.parts) * kDownColumns);
         return;
     }
     if (!one) return;
@@ -122,15 +126,16 @@ __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestTi
     *(u32x2*)(p.S + (int64_t)row * p.r + c) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
 }
 
-// A wave for every row up to 512 of them, whatever adapters they have, in workgroups of their own, which start sooner than those of eight waves: us, rows /
-// tiles: 3 rows, K = 1024 2.7 / 3.4; 64 rows of 48 adapters, K = 4096, r = 16 4.0 / 6.2; 200 rows of 106 adapters, r = 64 13.8 / 16.5.
+// Waves for single rows up to 512 of them, whatever adapters they have, in workgroups of their own, which start sooner than those of eight waves: us, rows /
+// tiles, with four columns to a wave: 3 rows, K = 1024 2.7 / 3.4; 64 rows of 48 adapters, K = 4096, r = 16 4.0 / 6.2; 200 rows of 106 adapters, r = 64 13.8 / 16.5.
+// With two: 2.7, 3.9, 12.4 (27 MB, 2.2 TB/s); 2048 rows on tiles 12.4 (17 MB of X).
 static hipError_t launch_request_down(const RequestDownArgs& a, hipStream_t st) {
     if (a.M <= 512) {
         hipLaunchKernelGGL(request_rows_kernel, dim3((unsigned)a.M, (unsigned)a.r / kDownColumns), dim3(64), 0, st, a);
         return hipGetLastError();
     }
     const RequestTileArgs t{a, (a.M + 15) / 16, a.r / 16};
-    const int64_t by_rows = ((int64_t)a.M * 4 * t.parts + kTileWaves - 1) / kTileWaves;
+    const int64_t by_rows = ((int64_t)a.M * (16 / kDownColumns) * t.parts + kTileWaves - 1) / kTileWaves;
     hipLaunchKernelGGL(request_tile_kernel, dim3((unsigned)((int64_t)t.tiles * t.parts + by_rows)), dim3(64 * kTileWaves), 0, st, t);
     return hipGetLastError();
 }
