@@ -126,11 +126,12 @@ __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestTi
     *(u32x2*)(p.S + (int64_t)row * p.r + c) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
 }
 
-// Waves for single rows up to 512 of them, whatever adapters they have, in workgroups of their own, which start sooner than those of eight waves: us, rows /
+// Waves for single rows up to 512 of them (r = 64: 256), whatever adapters they have, in workgroups of their own, which start sooner than those of eight waves: us, rows /
 // tiles, with four columns to a wave: 3 rows, K = 1024 2.7 / 3.4; 64 rows of 48 adapters, K = 4096, r = 16 4.0 / 6.2; 200 rows of 106 adapters, r = 64 13.8 / 16.5.
-// With two: 2.7, 3.9, 12.4 (27 MB, 2.2 TB/s); 2048 rows on tiles 12.4 (17 MB of X).
+// (Whole layer, 4096 -> 4096, one adapter: 128 rows, r = 16 15.5 / 21.6; 512 rows 28.0 / 31.7; r = 64, 256 rows 25.4 / 26.2, 512 rows 38.4 / 33.5; an adapter for
+// each row: level.)  With two: 2.7, 3.9, 12.4 (27 MB, 2.2 TB/s); 2048 rows on tiles 12.4 (17 MB of X).
 static hipError_t launch_request_down(const RequestDownArgs& a, hipStream_t st) {
-    if (a.M <= 512) {
+    if (a.M <= 512 && a.M * a.r <= 512 * 32) {
         hipLaunchKernelGGL(request_rows_kernel, dim3((unsigned)a.M, (unsigned)a.r / kDownColumns), dim3(64), 0, st, a);
         return hipGetLastError();
     }
