@@ -93,7 +93,7 @@ struct RopePasses {
     __host__ __device__ RopePasses(int H, int G) : of_q((H + HEADS - 1) / HEADS), all((H + HEADS - 1) / HEADS + (G + HEADS - 1) / HEADS) {}
 };
 
-template <int GL, bool INTER>
+template <int GL, bool INTER, bool PAST>
 __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
     const int64_t unit = (int64_t)blockIdx.x * (kRopeThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = unit / p.parts;
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
                 for (int i = 0; i < 8; ++i) y[i] = inv * (x[i] * cg[i] + o[i] * sg[i]);
                 u32x4 out = pack8(y);
                 if (!known) out = u32x4{0u, 0u, 0u, 0u};
-                if (ok[u]) *(u32x4*)(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j) = out;
+                if (ok[u]) put8<PAST>(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j, out);
             }
         }
     };
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
     heads(p.k + row * p.ldk, p.k_out + row * p.ldko, p.G, ps.all - ps.of_q, ps.first_k(part, p.parts), ck, sk);
 }
 
-template <int GL, bool INTER>
+template <int GL, bool INTER, bool PAST>
 __global__ void __launch_bounds__(64 * rope_bwd_waves(GL), rope_bwd_waves(GL)) rope_bwd_kernel(RopeArgs p) {
     constexpr int WAVES = rope_bwd_waves(GL);
     __shared__ float red[WAVES][2][GL * 8];
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(64 * rope_bwd_waves(GL), rope_bwd_waves(GL)) r
                     }
                     u32x4 out = pack8(dx);
                     if (!known) out = u32x4{0u, 0u, 0u, 0u};
-                    if (ok[u]) *(u32x4*)(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j) = out;
+                    if (ok[u]) put8<PAST>(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j, out);
                 }
             }
         };
@@ -274,6 +274,10 @@ static int rope_parts(int64_t M, int H, int G, bool backward) {
     const int64_t want = std::max((16 * kComputeUnits + M - 1) / std::max<int64_t>(M, 1), (int64_t)(backward ? (all + 2) / 4 | 1 : 1));
     return (int)std::min<int64_t>(want, all);
 }
+// Outputs of 16 MB and more go past the caches: ordinary stores leave them in the L2s, to be written back when the kernel ends.  us, stored / past the caches,
+// 32 + 8 heads of 128, by itself and with the reading of the outputs by another kernel behind it: 64 rows (0.7 MB) 9.6 / 9.6, 7.4 / 7.7; 512 (5 MB) 10.1 / 10.1
+// with it; 2048 (21 MB) 13.4 / 12.0, 22.1 / 21.5; 8192 (84 MB) 39.6 / 34.0, 58.5 / 59.7; backward, 8192 57.7 / 54.4.
+static bool past_caches(const RopeArgs& a) { return a.M * (a.H + a.G) * a.D * 2 >= 16 << 20; }
 template <class F>
 static auto with_lanes(int D, F&& f) {
     if (D <= 64) return f(std::integral_constant<int, 8>{});
@@ -281,13 +285,20 @@ static auto with_lanes(int D, F&& f) {
     return f(std::integral_constant<int, 32>{});
 }
 
+template <class F>
+static hipError_t with_flags(bool a, bool b, F&& f) {
+    if (a) return b ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
+    return b ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
+}
+
 hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st) {
     return with_lanes(a.D, [&](auto gl) {
         a.parts = rope_parts<gl()>(a.M, a.H, a.G, false);
         const int64_t blocks = (a.M * a.parts + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
-        if (interleaved) hipLaunchKernelGGL((rope_fwd_kernel<gl(), true>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
-        else hipLaunchKernelGGL((rope_fwd_kernel<gl(), false>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
-        return hipGetLastError();
+        return with_flags(interleaved, past_caches(a), [&](auto inter, auto past) {
+            hipLaunchKernelGGL((rope_fwd_kernel<gl(), inter(), past()>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
+            return hipGetLastError();
+        });
     });
 }
 
@@ -302,9 +313,10 @@ hipError_t launch_rope_bwd(RopeArgs a, bool interleaved, const RopeFinalizeArgs&
     if (f.blocks > 0) {
         const hipError_t e = with_lanes(a.D, [&](auto gl) {
             a.parts = rope_parts<gl()>(a.M, a.H, a.G, true);
-            if (interleaved) hipLaunchKernelGGL((rope_bwd_kernel<gl(), true>), dim3(f.blocks), dim3(64 * rope_bwd_waves(gl())), 0, st, a);
-            else hipLaunchKernelGGL((rope_bwd_kernel<gl(), false>), dim3(f.blocks), dim3(64 * rope_bwd_waves(gl())), 0, st, a);
-            return hipGetLastError();
+            return with_flags(interleaved, past_caches(a), [&](auto inter, auto past) {
+                hipLaunchKernelGGL((rope_bwd_kernel<gl(), inter(), past()>), dim3(f.blocks), dim3(64 * rope_bwd_waves(gl())), 0, st, a);
+                return hipGetLastError();
+            });
         });
         if (e != hipSuccess) return e;
     }
