@@ -2,6 +2,8 @@
 // the smallest that keeps its largest magnitude within 448: a scale that costs no rounding of its own, so that a value is rounded once, to
 // three fraction bits, and what is read back (value x scale) is exact in bf16.  Bound by HBM: 3 + 1 / D bytes an element (bf16: 4).  Eight
 // entries to a lane, a head to 8, 16 or 32 lanes, whose largest magnitude comes from the bit patterns (integers in the order of the values).
+// Measured: 2085 tokens of 8 heads of 128 to fp8, 13 MB, 5.5 us (slot, then the head: two latencies), 32768 tokens, 203 MB, 56 us; 29999 tokens read back from
+// fp8, 185 MB, 32 us.  Read with two or four heads to a lane, all their loads under way, and ordinary stores 48 us, with one 44.
 #include "lf_serve.h"
 
 namespace lf {

@@ -5,6 +5,8 @@
 // fp32, the result is rounded once.  Bound by HBM: 4 (6) bytes an element.  Eight entries to a lane (16-byte loads), 8, 16 or
 // 32 lanes to a head by its size; a head's sums are butterflies over its lanes.  With R's cosines and sines multiplied by gamma once per
 // row, y is one product and one multiply-add an entry; a pair's other entry comes from the lane that holds it, as the bf16 it was.
+// Measured (a copy of 2 GiB runs at 4.9 TB/s): forward, 8192 rows of 32 + 8 heads of 128, 168 MB, 34 us, 4.9 TB/s; backward, 5003 rows of 64 + 8, 277 MB, 53 us,
+// 5.2 TB/s, and 4.7 us for the sum of its planes; forward of 16 rows 4 us: the launch, and position, table and row read one after the other.
 #include <algorithm>
 
 #include "lf_serve.h"

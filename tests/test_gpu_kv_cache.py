@@ -126,3 +126,27 @@ def test_no_rows_and_arguments():
     for bad in ((k, v), (k, v, ke), (k, v.to(BF16), ke, ve), (k.float(), v.float()), (k[0], v[0], ke, ve), (k, v, ke[:1], ve)):
         with pytest.raises(AssertionError):
             binding.KVCache(*bad)
+
+
+@pytest.mark.parametrize("M,G,D,fp8", [(16500, 8, 128, True), (16500, 8, 128, False), (33000, 8, 64, True), (8300, 8, 256, True), (8300, 8, 208, False)])
+def test_large_reads(M, G, D, fp8):
+    """Outputs of more than 64 MB, which go past the caches, are those of reads of a thousand tokens (and, in bf16, what was written)."""
+    print("large reads", M, G, D, fp8, flush=True)
+    if D == 208:
+        M = 10200
+    page = 16
+    cache = binding.KVCache.empty(M // page + 1, page, G, D, fp8)
+    kv = torch.randn((M, 2, G, D), device="cuda").to(BF16)
+    slots = torch.randperm(M // page * page + page, device="cuda")[:M]
+    slots[5] = -1
+    binding.lora_kv_cache_write(cache, kv[:, 0], kv[:, 1], slots)
+    whole = binding.lora_kv_cache_read(cache, slots)
+    assert 2 * whole[0].numel() * 2 >= 64 << 20
+    for i in range(2):
+        for at in range(0, M, 1000):
+            piece = binding.lora_kv_cache_read(cache, slots[at:at + 1000])[i]
+            assert torch.equal(whole[i][at:at + 1000], piece)
+        assert not whole[i][5].any()
+        if not fp8:
+            kv[5] = 0
+            assert torch.equal(whole[i], kv[:, i])

@@ -196,3 +196,15 @@ def test_arguments():
     with pytest.raises(binding.LoraError):
         f(q[:, :3], cache, table, offsets, lens, 2, 30)
     assert f(q[:0], cache, table, torch.zeros(2, dtype=torch.int32, device="cuda"), lens, 0, 30).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("seqs,H,G,D,page,fp8,parts", [
+    ([(1, 40000)], 4, 1, 128, 16, True, 33), ([(2, 50000)], 8, 1, 64, 64, False, 65), ([(5, 21000), (1, 100), (3, 9000), (1, 513)], 4, 1, 128, 32, False, 33),
+    ([(150, 20000)], 2, 1, 128, 32, True, 5), ([(200, 9000), (70, 300), (129, 1)], 2, 1, 64, 16, False, 5)])
+def test_many_parts(seqs, H, G, D, page, fp8, parts):
+    """More parts than the join takes in one step, beside sequences of one part, which write their result themselves."""
+    q, cache, *_ = _setup(seqs, H, G, D, page, fp8, 4)
+    longest, new = max(kv for _, kv in seqs), max(n for n, _ in seqs)
+    rows = q.shape[0] * H
+    assert binding.alloc_paged_attn_workspace(cache, q.shape[0], H, len(seqs), new, longest).numel() >= parts * rows * (4 * D + 8)
+    _check(seqs, H, G, D, page, fp8, seed=4)

@@ -136,3 +136,11 @@ def test_arguments():
             f(*bad)
     with pytest.raises(binding.LoraError):
         f(q, k, gq, gk, cos, sin, pos, eps=0.0)
+
+
+@pytest.mark.parametrize("M,H,G,D,rot,inter", [(2100, 24, 8, 128, 128, False), (2100, 24, 8, 128, 64, True), (4200, 24, 8, 64, 64, False),
+                                               (4200, 30, 2, 64, 32, True), (4200, 6, 2, 256, 256, False), (4200, 7, 1, 256, 128, True)])
+def test_large_outputs(M, H, G, D, rot, inter):
+    """Outputs of more than 16 MB, which go past the caches; backward with several parts of rows to a wave."""
+    test_forward(M, H, G, D, rot, inter)
+    test_backward(M, H, G, D, rot, inter)

@@ -140,3 +140,10 @@ def test_arguments():
         binding.lora_requests_fwd(X, W, A, B, ids[:4], s)
     Y, S = binding.lora_requests_fwd(X[:0], W, A, B, ids[:0], s)
     assert Y.shape == (0, 64) and S.shape == (0, 16)
+
+
+@pytest.mark.parametrize("M,r", [(255, 64), (256, 64), (257, 64), (400, 64), (512, 32), (513, 32), (512, 16)])
+def test_first_product_by_rows_or_tiles(M, r):
+    """Both sides of the line between single rows and tiles of rows in the first product."""
+    for ids in ("one", "chunks", "any"):
+        _check(_case(M, 704, 192, r, 6, ids, True, M + r), (M, r, ids))
