@@ -931,16 +931,16 @@ AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, 
     if (window) keys = std::min<int64_t>(keys, (int64_t)window + (pl.rows + group - 1) / group + 16);
     // Parts, until there are so many workgroups to a compute unit, of so many keys and more.  Sequences differ in length, which only the device knows, so
     // that a batch of long ones takes more.  Few rows: one sequence 2, of 512; a batch 4, and 8 of 2048.  Many rows, whose parts' results cost 1 KB a row
-    // (D = 128) to write and read again: one, of 256; 2, of 1024; a batch 8, of 1536.  us, this rule / others: few rows, four sequences of 33000 - 131072
+    // (D = 128) to write and read again: one, of 256; 2, of 1024; a batch 8, of 1536, up to 16 parts.  us, this rule / others: few rows, four sequences of 33000 - 131072
     // keys 236 / 253 (4 to a compute unit), eight of 3000 - 65536 210 / 235 (4), 32 of 200 - 4000 36.9 / 37.8 (8, of 512), 128 of 500 - 3000 173 / 179 (8, of 512), one
     // of 131072 56 / 62 (4); many rows, two of 5003 and 16000, 1021 new 283 / 319 (4), four of 600 - 6000, 300 new 116 / 132 (of 4096), eight of 1000 - 2048, 512
     // new 144 / 207 (of 1024), 16 of 100 - 1000, 64 new 39 / 43 (2, of 512), one of 8192, 1024 new 148 / 154 (4, of 2048), two of 2000 - 3000, 60 new, D = 64
-    // 18 / 19 (of 512).
+    // 18 / 19 (of 512), four of 12000 - 61000, 47 new 172 / 178 (39 parts).
     const int64_t have = std::max<int64_t>(tiles * B * G, 1);
     const auto up_to = [&](int per_unit, int64_t least) { return std::min<int64_t>(per_unit * kComputeUnits / have, keys / least); };
     int64_t parts = 1;
     if (pl.rows < 128) parts = B > 1 ? std::max(up_to(4, 512), up_to(8, 2048)) : up_to(2, 512);
-    else parts = std::max({up_to(1, 256), up_to(2, 1024), B > 1 ? up_to(8, 1536) : 1});
+    else parts = std::max({up_to(1, 256), up_to(2, 1024), B > 1 ? std::min<int64_t>(up_to(8, 1536), 16) : 1});
     parts = std::max<int64_t>(1, parts);
     const int64_t step = 128;
     pl.split_keys = (int)(((keys + parts - 1) / parts + step - 1) / step * step);

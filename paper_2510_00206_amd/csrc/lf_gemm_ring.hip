@@ -299,7 +299,7 @@ __device__ __forceinline__ void ring_stage(f32x4 (&acc)[C::MI][C::NI], const Rin
 // alone, DEPTH steps ahead, with no branch around the loads (see ask); S is held in registers.  The steps stand in a list in LDS.  The first of them
 // are asked for before the base product where the registers can hold them through it (LATE; the small tiles: 16 rows to a wave), and come in
 // meanwhile; elsewhere the whole term comes before the base product, while the copying waves fill the ring.  Bound by the latency of B's
-// lines, of which the registers allow four to seven steps under way: 200 rows of 106 adapters, mean rank 37 of 64, 4096 -> 14336: 260 MB, 80 us, of which the
+// lines, of which the registers allow four to eight steps under way: 200 rows of 106 adapters, mean rank 37 of 64, 4096 -> 14336: 260 MB, 80 us, of which the
 // base product is 39.  us, whole layer, against loads behind branches, whose waits were for all of them, and a list made adapter by adapter: that 103 / 97;
 // 64 rows of 48 adapters, r = 16, 4096 -> 6144 19.4 / 17.6; 384 rows of 170, r = 64, 4096 -> 4096 101 / 80; 200 rows, r = 16, 4096 -> 14336 63 / 54;
 // 128 rows, r = 32, 4096 -> 4096 27.5 / 25.2.  Steps between the slabs of the base product, two or three ahead, were slower: 103, 21.5, 92, 60, 26.4.
