@@ -184,9 +184,9 @@ __global__ void __launch_bounds__(64 * rope_bwd_waves(GL), rope_bwd_waves(GL)) r
                     const int head = (first + u * p.parts) * ps.HEADS + ln.slot;
                     ok[u] = ln.active && head < n;
                     xr[u] = dr[u] = u32x4{0u, 0u, 0u, 0u};
-                    if (ok[u]) {
+                    if (ok[u] && known) {                  // (a row outside the tables may hold infinities and NaN, and 0 times those is NaN)
                         xr[u] = *(const u32x4*)(x_row + (int64_t)head * p.D + 8 * ln.j);
-                        if (known) dr[u] = *(const u32x4*)(dy_row + (int64_t)head * p.D + 8 * ln.j);
+                        dr[u] = *(const u32x4*)(dy_row + (int64_t)head * p.D + 8 * ln.j);
                     }
                 }
 #pragma unroll

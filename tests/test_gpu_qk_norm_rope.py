@@ -144,3 +144,30 @@ def test_large_outputs(M, H, G, D, rot, inter):
     """Outputs of more than 16 MB, which go past the caches; backward with several parts of rows to a wave."""
     test_forward(M, H, G, D, rot, inter)
     test_backward(M, H, G, D, rot, inter)
+
+
+@pytest.mark.parametrize("M,H,G,D,rot,inter", [(4, 3, 2, 64, 64, False), (40, 32, 8, 128, 128, False), (33, 4, 1, 256, 256, True), (50, 6, 2, 96, 48, False),
+                                               (1500, 9, 2, 48, 32, True), (4500, 26, 2, 128, 128, False)])
+def test_rows_outside_the_tables_add_nothing(M, H, G, D, rot, inter):
+    """Rows of padding over memory that holds anything: zeros in dq and dk, and dgamma of the other rows alone (test_backward's bounds)."""
+    print("rows outside", M, H, G, D, rot, inter, flush=True)
+    _, q, k, gq, gk, cos, sin, pos = _inputs(M, H, G, D, rot, 77 + M)
+    g = gen(M)
+    xs, dys = [q.clone(), k.clone()], [normal(g, (M, H, D)), normal(g, (M, G, D))]
+    out = torch.arange(M) % 3 == 1
+    pos[out] = torch.tensor([-1, 50, 1 << 30, -(1 << 31)], dtype=torch.int32)[torch.arange(int(out.sum())) % 4]
+    for t in xs + dys:
+        t[out] = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38], dtype=BF16)[torch.randint(0, 4, t[out].shape, generator=g)]
+    got = binding.lora_qk_norm_rope_bwd(*(t.cuda() for t in (*xs, gq, gk, cos, sin, pos, *dys)), eps=1e-5, interleaved=inter)
+    for i, gamma in enumerate((gq, gk)):
+        x, gamma, dy = xs[i][~out].to(F64).requires_grad_(), gamma.to(F64).requires_grad_(), dys[i][~out].to(F64)
+        dx, dg = torch.autograd.grad(norm_rope(x, gamma, cos, sin, pos[~out], 1e-5, inter)[0], (x, gamma), dy)
+        with torch.no_grad():
+            inv = 1 / torch.sqrt((x * x).mean(-1, keepdim=True) + 1e-5)
+            e = 2 * dy.abs().amax(-1, keepdim=True)
+            u = e * gamma.abs()
+            mag = inv * (u + (x * inv).abs() * (u * (x * inv).abs()).mean(-1, keepdim=True))
+            mag_g = (e * (x * inv).abs()).sum((0, 1))
+        assert not got[i][out.cuda()].any()
+        within(got[i][(~out).cuda()], dx, U16 * dx.abs() + (D + 32) * U32 * mag, ("dx", i))
+        within(got[2 + i], dg, (D + 64 + 512) * U32 * mag_g, ("dgamma", i))
