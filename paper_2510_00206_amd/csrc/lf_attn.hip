@@ -24,7 +24,8 @@
 
 namespace lf {
 
-constexpr float kNone = -1e30f;                  // reference of a row that has seen nothing: finite, so that every p against it is 0 and no case of its own
+constexpr float kNone = -__FLT_MAX__;             // reference of a row that has seen nothing: finite, so that every p against it is 0 and no case of its own
+constexpr float kFar = 0x1p20f;                  // the largest reference that p is formed against in one step (move_base)
 
 // What a workgroup works on.
 struct AttnTile {
@@ -157,6 +158,45 @@ __device__ __forceinline__ bool follow(const float (&top)[NQ], float (&m)[NQ], f
     }
     return true;
 }
+// References past kFar.  p_of takes the scaled score exactly, m is rounded: past 2^24 their difference is no longer near 0 for the largest score itself, and past 2^31
+// its power of two is infinity or 0.  Such a row counts its scores from one of them (base: a float for every query of the wave, in LDS, read
+// where far is set; zero for the other rows) and m from there on, so that the largest score's difference is exact.  Rare: a branch a step on a
+// scalar, and nothing kept in registers (us, without / with: 278 / 278.5 for the chunks below, 343.9 / 344.9 over an fp8 cache, 61.3 / 62.5 for 16 x 6 tokens over
+// up to 9000 keys, fp8, long single tokens level).
+template <int NQ, int KB>
+__device__ __forceinline__ void count_from_base(f32x4 (&s)[NQ][KB], float (&top)[NQ], const float* base, int c) {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const float d = base[16 * i + c];
+        top[i] -= d;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) s[i][b] -= d;
+    }
+}
+// Behind follow(), where it has moved a reference.
+template <int NQ, int KB>
+__device__ __forceinline__ void move_base(f32x4 (&s)[NQ][KB], const float (&top)[NQ], float (&m)[NQ], float* base, int c, int& far) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) any |= fabsf(m[i]) > kFar && m[i] != kNone;
+    if (__builtin_expect(!__any(any), 1)) return;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const bool moves = fabsf(m[i]) > kFar && m[i] != kNone;
+        const float d = moves ? top[i] : 0.f;
+        base[16 * i + c] = far ? base[16 * i + c] + d : d;           // (the four lanes of a query write the same)
+        m[i] = moves ? 0.f : m[i];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) s[i][b] -= d;
+    }
+    far = 1;
+}
+// The references as the other waves and parts know them, from 0.
+template <int NQ>
+__device__ __forceinline__ void count_from_zero(float (&m)[NQ], const float* base, int c, float scale) {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) m[i] = __builtin_fmaf(base[16 * i + c], scale, m[i]);
+}
 __device__ __forceinline__ float p_of(float s, float scale, float m) { return __builtin_amdgcn_exp2f(__builtin_fmaf(s, scale, -m)); }
 
 // The lane's number, formed where it is asked for: in code that runs rarely, or after a loop, so that nothing derived from it is kept through the loop.
@@ -287,7 +327,7 @@ struct Few {
     static constexpr int VL = KEYS * D * (FP8 ? 1 : 2) / 1024;     // ... for the values
     static constexpr int V_BYTES = KEYS * D * 2, O_BYTES = 16 * NQ * D * 4;
     static constexpr int WAVE_LDS = V_BYTES > O_BYTES ? V_BYTES : O_BYTES;
-    static constexpr int LDS = WAVES * WAVE_LDS + WAVES * NQ * 16 * 8;
+    static constexpr int BASE = WAVES * WAVE_LDS + WAVES * NQ * 16 * 8, LDS = BASE + WAVES * NQ * 16 * 4;
 };
 
 template <int D, bool FP8, int NQ>
@@ -299,6 +339,8 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
     if (!attn_tile<16 * NQ>(p, t)) return;
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = l & 15, q = l >> 4;
     char* mine = smem + w * C::WAVE_LDS;
+    float* base = (float*)(smem + C::BASE) + w * NQ * 16;
+    int far = 0;
 
     // queries: step kk holds entries 32 kk + 8 q .. + 7, fp8 64 (kk / 2) + 16 q + 8 (kk & 1) .. + 7 (as a 16-byte load of a key brings them)
     bf16x8 qf[NQ][KK];
@@ -431,13 +473,16 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
             if (!whole) hide(s[i], key, pos[i], p.window);
             top[i] = top_of<2>(s[i]);
         }
-        if (follow<NQ>(top, m, back, p.scale))
+        if (__builtin_expect(far, 0)) count_from_base(s, top, base, lane_here() & 15);
+        if (follow<NQ>(top, m, back, p.scale)) {
+            move_base(s, top, m, base, lane_here() & 15, far);
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
                 sum[i] *= back[i];
 #pragma unroll
                 for (int d = 0; d < DB; ++d) o[i][d] *= back[i];
             }
+        }
         bf16x8 pf[NQ];
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
@@ -456,6 +501,7 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
     }
 
     // the four waves' sums, brought to one reference
+    if (far) count_from_zero(m, base, c, p.scale);
     float* ml = (float*)(smem + C::WAVES * C::WAVE_LDS);              // [row][wave] of m, then of l
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
@@ -513,7 +559,8 @@ constexpr int slots_before(int n, int items, int slots) { return n <= 0 ? 0 : n 
 template <int D, bool FP8>
 struct Many {
     static constexpr int KEYS = 64, ROWS = 128, NQ = 2;
-    static constexpr int TILE = KEYS * D * 2, FLAGS = 4 * TILE, RAW = FLAGS + 16;      // two tiles of keys, two of values; flags; fp8 a tile as it is held
+    // two tiles of keys, two of values; flags; of every row the score that it counts from; fp8 a tile as it is held
+    static constexpr int TILE = KEYS * D * 2, FLAGS = 4 * TILE, BASE = FLAGS + 16, RAW = BASE + ROWS * 4;
     static constexpr int LDS = RAW + (FP8 ? KEYS * D : 0);
 };
 
@@ -627,6 +674,8 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
     const int first_pos = pos_of(p, t, t.row0), last_pos = pos_of(p, t, t.row0 + t.rows - 1);
     auto all_whole = [&](int key) { return key + C::KEYS - 1 <= first_pos && (!p.window || key > last_pos - p.window); };
     int* flags = (int*)(smem + C::FLAGS);
+    float* base = (float*)(smem + C::BASE) + 32 * w;
+    int far = 0;
     auto brought_v = [&](int key, int stage) {
         char* st = smem + 2 * C::TILE + stage * C::TILE;
         const bool guard = !all_whole(key);
@@ -764,7 +813,9 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
                 hide(s[i], key, pos[i], p.window);
                 top[i] = top_of<KB>(s[i]);
             }
+        if (__builtin_expect(far, 0)) count_from_base(s, top, base, lane_here() & 15);
         const bool moved = follow<NQ>(top, m, back, p.scale);
+        if (moved) move_base(s, top, m, base, lane_here() & 15, far);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) add[i] = 0.f;
         __builtin_amdgcn_sched_barrier(0);
@@ -831,6 +882,7 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
         for (int n = 0; n < NV; ++n) value(wb, n);
         if (flags[1] == key - C::KEYS) add_not_finite<D, FP8, NQ, KB>(p, t, o, pos, key - C::KEYS);
     }
+    if (far) count_from_zero(m, base, lane_here() & 15, p.scale);
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
         const float total = over_quarters(sum[i], [](float a, float b) { return a + b; });

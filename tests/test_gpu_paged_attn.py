@@ -1,10 +1,12 @@
 """Attention over the paged cache against the 64-bit form: lengths from one token, ragged batches, every grouping of heads and kernel form, windows,
 rows that see nothing, and anything at all in the cache behind a sequence's end."""
+import math
+
 import pytest
 import torch
 
 from paper_2510_00206_amd import binding
-from serve_util import BF16, F64, attention, gen, normal, quantised, widened, within
+from serve_util import BF16, F64, U16, U32, attention, gen, normal, quantised, widened, within
 
 pytestmark = pytest.mark.gpu
 NAN = float("nan")
@@ -208,3 +210,57 @@ def test_many_parts(seqs, H, G, D, page, fp8, parts):
     rows = q.shape[0] * H
     assert binding.alloc_paged_attn_workspace(cache, q.shape[0], H, len(seqs), new, longest).numel() >= parts * rows * (4 * D + 8)
     _check(seqs, H, G, D, page, fp8, seed=4)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("n,kv,H,G,D", [(1, 700, 4, 2, 64), (1, 40, 2, 2, 128), (7, 300, 4, 1, 128), (12, 90, 4, 2, 64), (70, 333, 2, 1, 128), (150, 900, 4, 2, 64), (3, 20000, 4, 1, 128)])
+@pytest.mark.parametrize("size", [2.0 ** 20, 2.0 ** 32, 2.0 ** 60, 2.0 ** 110])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_large_scores(n, kv, H, G, D, fp8, size, sign):
+    """Scores of any size that fp32 holds.  Keys are one of three multiples of one vector, so that a row's scores are three numbers as far apart as they are
+    large, exact in fp32: the result is the mean of the values of the visible keys with the largest.  The weights of these are equal, and their rounding to bf16
+    too: what is left are the result's rounding and the sums."""
+    print("large scores", n, kv, H, G, D, fp8, size, sign, flush=True)
+    q, cache, table, offsets, lens, held = _setup([(n, kv)], H, G, D, 16, fp8, n + kv, junk=False)
+    root = 2.0 ** math.floor(math.log2(size) / 2)
+    level = torch.randint(1, 4, (kv, G), generator=gen(kv))
+    level[:min(kv, 60)] = 2                                  # (references that move on the way, up or, with sign < 0, sometimes not at all)
+    q = torch.full_like(q, sign * root)
+    base = size / root
+    k, ke, page = cache.tensors[0], cache.tensors[2], cache.page
+    j = torch.arange(kv)
+    at = table[0, j // page].long()
+    if fp8:
+        hk, he = k.view(torch.uint8).cpu(), ke.cpu()
+        hk[at, :, j % page] = (level.float()[..., None].expand(kv, G, D)).to(torch.float8_e4m3fn).view(torch.uint8)
+        he[at, :, j % page] = 127 + int(math.log2(base))
+        k.view(torch.uint8).copy_(hk), ke.copy_(he)
+    else:
+        hk = k.cpu()
+        hk[at, :, j % page] = (level.to(F64)[..., None] * base).expand(kv, G, D).to(BF16)
+        k.copy_(hk)
+    out = binding.lora_paged_attn_fwd(q.cuda(), cache, table.cuda(), offsets.cuda(), lens.cuda(), n, kv)
+    v = held[0][1]
+    ref, mag = torch.zeros((n, H, D), dtype=F64), torch.zeros((n, H, D), dtype=F64)
+    for i in range(n):
+        for h in range(H):
+            see = level[:kv - n + i + 1, h // (H // G)]
+            top = see == (see.max() if sign > 0 else see.min())
+            w = v[:kv - n + i + 1, h // (H // G)][top]
+            ref[i, h], mag[i, h] = w.mean(0), w.abs().mean(0)
+    within(out, ref, U16 * ref.abs() + (kv + 16) * U32 * mag, (n, kv, H, G, D, fp8, size, sign))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_large_scores_of_ordinary_inputs(fp8):
+    """Scores far past what exponentials hold, none of them equal: every result is one of the visible keys' values or lies between them."""
+    for n, kv, H, G, D in ((1, 500, 4, 2, 128), (9, 400, 4, 2, 64), (130, 600, 2, 1, 128)):
+        q, cache, table, offsets, lens, held = _setup([(n, kv)], H, G, D, 16, fp8, 3, std=1.0 if fp8 else 3e7)
+        out = binding.lora_paged_attn_fwd((q * 1e8).cuda(), cache, table.cuda(), offsets.cuda(), lens.cuda(), n, kv).cpu().to(F64)
+        v = held[0][1]
+        for i in range(n):
+            for h in range(H):
+                see = v[:kv - n + i + 1, h // (H // G)]
+                lo, hi = see.amin(0), see.amax(0)
+                slack = 2 * U16 * see.abs().amax(0)
+                assert bool(((out[i, h] >= lo - slack) & (out[i, h] <= hi + slack)).all()), (n, i, h, fp8)
