@@ -288,6 +288,10 @@ __device__ __forceinline__ const lora_bf16* q_row(const AttnArgs& p, const AttnT
     return p.q + (int64_t)(t.first + tok) * p.ldq + (int64_t)(t.g * p.group + row - tok * p.group) * p.c.D;
 }
 
+// Token `tok` is one of more than there are keys: its row sees none and is zeros.  Every other row sees its own token's key: if all scores that it
+// sees are -infinity its sum is 0 as well, and the result NaN, 0 / 0.
+__device__ __forceinline__ bool sees_nothing(const AttnTile& t, int tok) { return t.kv - t.n + tok < 0; }
+
 // Four entries from `d` on of a finished row: o = sum of p v, l = sum of p, m = their reference.
 __device__ __forceinline__ void put(const AttnArgs& p, const AttnTile& t, int row, int d, f32x4 o, float m, float l) {
     const int tok = row / p.group, head = t.g * p.group + row - tok * p.group;
@@ -300,7 +304,7 @@ __device__ __forceinline__ void put(const AttnArgs& p, const AttnTile& t, int ro
         }
         return;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;             // a row that sees nothing: zeros
+    const float inv = sees_nothing(t, tok) ? 0.f : 1.f / l;
     u32x2 v;
     v.x = pack_bf16x2(o[0] * inv, o[1] * inv);
     v.y = pack_bf16x2(o[2] * inv, o[3] * inv);
@@ -967,7 +971,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs p) {
             sum += red_ml[i][1] * f;
         }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = sees_nothing(t, tok) ? 0.f : 1.f / sum;
     *(u32x2*)(p.out + (int64_t)(t.first + tok) * p.ldo + (int64_t)head * D + d) =
         u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
 }

@@ -264,3 +264,25 @@ def test_large_scores_of_ordinary_inputs(fp8):
                 lo, hi = see.amin(0), see.amax(0)
                 slack = 2 * U16 * see.abs().amax(0)
                 assert bool(((out[i, h] >= lo - slack) & (out[i, h] <= hi + slack)).all()), (n, i, h, fp8)
+
+
+@pytest.mark.parametrize("n,kv,parts", [(1, 60, False), (2, 3000, True), (70, 200, False), (140, 2500, True)])
+def test_scores_of_minus_infinity(n, kv, parts):
+    """Keys of infinite size against a query of the other sign: a row that sees such keys only has no softmax (0 / 0), unlike one that sees none;
+    one that sees another key too has that key's."""
+    H, G, D = 2, 1, 64
+    q, cache, table, offsets, lens, held = _setup([(n, kv)], H, G, D, 16, False, 6, junk=False)
+    assert (binding.alloc_paged_attn_workspace(cache, n, H, 1, n, kv).numel() > 256) == parts
+    q = q.abs()
+    q[..., 0] = 1.0
+    cache.tensors[0][..., 0] = -float("inf")
+    args = (table.cuda(), offsets.cuda(), lens.cuda(), n, kv)
+    out = binding.lora_paged_attn_fwd(q.cuda(), cache, *args)
+    assert bool(torch.isnan(out).all())
+    at = kv - n // 2 - 1                                     # the rows from n // 2 on ... see this one
+    cache.tensors[0][int(table[0, at // 16]), 0, at % 16] = 0
+    out = binding.lora_paged_attn_fwd(q.cuda(), cache, *args).cpu()
+    first = n - 1 - n // 2
+    assert bool(torch.isnan(out[:first]).all())
+    v = held[0][1][at, 0].to(BF16)
+    assert torch.equal(out[first:], v.expand(n - first, H, D))
