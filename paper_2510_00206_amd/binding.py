@@ -495,6 +495,7 @@ def lora_kv_cache_read(cache: KVCache, slots, k=None, v=None):
 
 
 def alloc_paged_attn_workspace(cache: KVCache, T, H, seqs, max_new, max_kv, window=0, device="cuda") -> torch.Tensor:
+    """For steps of at most T tokens of at most seqs sequences, max_new tokens of each and max_kv keys."""
     n = int(load_library().lora_paged_attn_workspace_bytes(cache._ref, T, H, seqs, max_new, max_kv, window))
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 

@@ -977,14 +977,38 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs p) {
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
+// The most keys that a tile sees.
+static int64_t keys_of_tile(int rows, int group, int64_t max_kv, int window) {
+    return window ? std::min<int64_t>(max_kv, (int64_t)window + (rows + group - 1) / group + 16) : max_kv;
+}
+// Parts of a range (plan_attn): as many as make per_unit workgroups to a compute unit, of `least` keys and more, at most `most`; `one`: for one sequence (many
+// rows: for a batch too), otherwise for a batch.
+struct PartsRule { bool few, one; int per_unit, least, most; };
+constexpr PartsRule kParts[] = {{true, true, 2, 512, 1 << 30}, {true, false, 4, 512, 1 << 30}, {true, false, 8, 2048, 1 << 30},
+                                {false, true, 1, 256, 1 << 30}, {false, true, 2, 1024, 1 << 30}, {false, false, 8, 1536, 16}};
+
+// Rows of partial results (parts x T x H) that no step of at most these sizes exceeds, though a smaller one is cut into more parts.  Of T <= B * max_new tokens in
+// `tiles` of so many rows a sequence, c workgroups to a compute unit make c * kComputeUnits / (tiles * B * G) parts or fewer: parts x T x H is at most c * kComputeUnits
+// rows times those of a sequence (few rows) or of a tile (many), and at most T x H times the parts that one sequence and one tile have.
+int64_t attn_part_rows(int64_t T, int B, int G, int group, int max_new, int64_t max_kv, int window) {
+    int64_t rows = 0;
+    for (const PartsRule& u : kParts) {
+        if (u.few ? group > 32 : (int64_t)max_new * group <= 32) continue;
+        if (B == 1 && !u.one) continue;
+        const int64_t units = (int64_t)u.per_unit * kComputeUnits;
+        const int64_t of_seq = u.few ? std::min<int64_t>((int64_t)max_new * group, 32) / group * group : 128;
+        const int64_t parts = std::min<int64_t>({units / G, keys_of_tile(u.few ? 32 : 128, group, max_kv, window) / u.least, u.most});
+        if (parts > 1) rows = std::max(rows, std::min(units * of_seq, parts * T * G * group));
+    }
+    return rows;
+}
+
 AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, int window) {
     AttnPlan pl;
     const int64_t rows = (int64_t)max_new * group;
     pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
     const int64_t tiles = (rows + pl.rows - 1) / pl.rows;
-    // the most keys that a tile sees
-    int64_t keys = max_kv;
-    if (window) keys = std::min<int64_t>(keys, (int64_t)window + (pl.rows + group - 1) / group + 16);
+    const int64_t keys = keys_of_tile(pl.rows, group, max_kv, window);
     // Parts, until there are so many workgroups to a compute unit, of so many keys and more.  Sequences differ in length, which only the device knows, so
     // that a batch of long ones takes more.  Few rows: one sequence 2, of 512; a batch 4, and 8 of 2048.  Many rows, whose parts' results cost 1 KB a row
     // (D = 128) to write and read again: one, of 256; 2, of 1024; a batch 8, of 1536, up to 16 parts.  us, this rule / others: few rows, four sequences of 33000 - 131072
@@ -995,9 +1019,8 @@ AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, 
     const int64_t have = std::max<int64_t>(tiles * B * G, 1);
     const auto up_to = [&](int per_unit, int64_t least) { return std::min<int64_t>(per_unit * kComputeUnits / have, keys / least); };
     int64_t parts = 1;
-    if (pl.rows < 128) parts = B > 1 ? std::max(up_to(4, 512), up_to(8, 2048)) : up_to(2, 512);
-    else parts = std::max({up_to(1, 256), up_to(2, 1024), B > 1 ? std::min<int64_t>(up_to(8, 1536), 16) : 1});
-    parts = std::max<int64_t>(1, parts);
+    for (const PartsRule& u : kParts)
+        if (u.few == (pl.rows < 128) && (u.one ? B == 1 || !u.few : B > 1)) parts = std::max(parts, std::min<int64_t>(up_to(u.per_unit, u.least), u.most));
     const int64_t step = 128;
     pl.split_keys = (int)(((keys + parts - 1) / parts + step - 1) / step * step);
     if (pl.split_keys < step) pl.split_keys = step;

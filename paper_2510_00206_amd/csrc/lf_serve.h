@@ -60,6 +60,7 @@ hipError_t launch_rope_bwd(RopeArgs a, bool interleaved, const RopeFinalizeArgs&
 hipError_t launch_cache_write(const CacheCopyArgs& a, hipStream_t st);
 hipError_t launch_cache_read(const CacheCopyArgs& a, hipStream_t st);
 AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, int window);
+int64_t attn_part_rows(int64_t T, int B, int G, int group, int max_new, int64_t max_kv, int window);      // of any step of at most these sizes
 hipError_t launch_attn(AttnArgs a, const AttnPlan& p, int max_new, hipStream_t st);
 hipError_t launch_requests(const RequestArgs& a, hipStream_t st);
 

@@ -69,9 +69,8 @@ lora_status check_attn(const PagedCache& c, int64_t T, int32_t H, int64_t B, int
     return LORA_OK;
 }
 
-size_t attn_scratch(const AttnPlan& pl, int64_t T, int32_t H, int32_t D) {
-    return pl.splits == 1 ? 0 : align_up((size_t)pl.splits * T * H * D * 4) + align_up((size_t)pl.splits * T * H * 8);
-}
+size_t attn_scratch(size_t part_rows, int32_t D) { return align_up(part_rows * D * 4) + align_up(part_rows * 8); }
+size_t attn_scratch(const AttnPlan& pl, int64_t T, int32_t H, int32_t D) { return pl.splits == 1 ? 0 : attn_scratch((size_t)pl.splits * T * H, D); }
 
 }  // namespace
 
@@ -154,7 +153,10 @@ size_t lora_paged_attn_workspace_bytes(const lora_kv_cache* cache, int64_t T, in
     PagedCache c;
     if (paged(cache, c) != LORA_OK || check_attn(c, T, H, B, max_new, max_kv, window) != LORA_OK) return 0;
     if (T == 0 || B == 0 || max_new == 0) return 256;
-    return std::max<size_t>(256, attn_scratch(plan_attn((int)B, c.heads, H / c.heads, c.D, (int)max_new, max_kv, window), T, H, c.D));
+    const int group = H / c.heads;
+    // (its own plan too: more tokens than sequences of max_new can have are allowed)
+    return std::max({(size_t)256, attn_scratch(plan_attn((int)B, c.heads, group, c.D, (int)max_new, max_kv, window), T, H, c.D),
+                     attn_scratch((size_t)attn_part_rows(T, (int)B, c.heads, group, (int)max_new, max_kv, window), c.D)});
 }
 
 lora_status lora_paged_attn_fwd(const lora_bf16* q, const lora_kv_cache* cache, const int32_t* table, const int32_t* offsets, const int32_t* kv_lens,

@@ -286,3 +286,15 @@ def test_scores_of_minus_infinity(n, kv, parts):
     assert bool(torch.isnan(out[:first]).all())
     v = held[0][1][at, 0].to(BF16)
     assert torch.equal(out[first:], v.expand(n - first, H, D))
+
+
+def test_one_workspace_for_smaller_steps():
+    """A workspace for the largest step serves those of fewer tokens, sequences and keys, though these are cut into more parts."""
+    cache = _setup([(1, 16)], 32, 8, 128, 16, False, 1)[1]
+    ws = binding.alloc_paged_attn_workspace(cache, 256, 32, 64, 64, 20000)
+    for seqs in ([(4, 20000)] * 2, [(1, 20000)], [(4, 9000)] * 8, [(30, 17000), (1, 400)], [(64, 20000)] * 2, [(1, 3000)] * 5, [(3, 7)] * 64):
+        q, cache, table, offsets, lens, held = _setup(seqs, 32, 8, 128, 16, False, len(seqs))
+        new, longest = max(n for n, _ in seqs), max(kv for _, kv in seqs)
+        print("one workspace", seqs[:2], len(seqs), flush=True)
+        args = (q.cuda(), cache, table.cuda(), offsets.cuda(), lens.cuda(), new, longest)
+        assert torch.equal(binding.lora_paged_attn_fwd(*args, workspace=ws), binding.lora_paged_attn_fwd(*args))

@@ -1,6 +1,7 @@
 """The entry points around served adapters refuse bad arguments on the host, before anything is enqueued, with the documented status."""
 import ctypes as C
 import os
+import random
 
 import pytest
 
@@ -117,3 +118,18 @@ def test_attention_workspace(lib):
     n = need(1, 32, 1, 1, 131072)
     call = lambda size: lib.lora_paged_attn_fwd(p, c, p, p, p, 1, 32, 1, 10000, 4096, 10000, 4096, 1, 131072, 0.1, 0, p, p, size, None)
     assert call(n - 1) == WORKSPACE
+
+
+def test_attention_workspace_serves_smaller_steps(lib):
+    """What the query returns never falls as a step grows: one workspace, for the largest, is enough for all."""
+    rng = random.Random(5)
+    size = lambda lo, hi: int(round(lo * (hi / lo) ** rng.random()))
+    for _ in range(3000):
+        heads, dim = rng.choice((1, 2, 8, 16)), rng.choice((64, 128))
+        c, H, window = _cache(dim=dim, heads=heads), heads * rng.choice((1, 4, 7, 16, 40)), rng.choice((0, 0, size(1, 20000)))
+        B, new, kv = size(1, 200), size(1, 2000), size(1, 150000)
+        T = size(1, B * new)
+        B1, new1, kv1 = size(1, B), size(1, new), size(1, kv)
+        T1 = size(1, min(T, B1 * new1))
+        large, small = (lib.lora_paged_attn_workspace_bytes(c, t, H, b, n, k, window) for t, b, n, k in ((T, B, new, kv), (T1, B1, new1, kv1)))
+        assert 256 <= small <= large, (heads, dim, H, window, (T, B, new, kv), (T1, B1, new1, kv1))
