@@ -4,6 +4,8 @@
 // The first is bound by the latency of ids, ranks and adapters, one after the other, and by the reading of the adapters: a wave takes two columns of the
 // rank for one row, so that a decode step of a few rows is spread over the chip, or, where many rows come as chunks of few requests, 16 rows
 // go through MFMAs at once.  Two launches: with S formed in the tiles of the second product every column tile would form it again.
+#include <algorithm>
+
 #include "lf_gemm_parts.h"
 #include "lf_gemm_ring.h"
 #include "lf_serve.h"
@@ -135,10 +137,18 @@ static hipError_t launch_request_down(const RequestDownArgs& a, hipStream_t st) 
         hipLaunchKernelGGL(request_rows_kernel, dim3((unsigned)a.M, (unsigned)a.r / kDownColumns), dim3(64), 0, st, a);
         return hipGetLastError();
     }
-    const RequestTileArgs t{a, (a.M + 15) / 16, a.r / 16};
-    const int64_t by_rows = ((int64_t)a.M * (16 / kDownColumns) * t.parts + kTileWaves - 1) / kTileWaves;
-    hipLaunchKernelGGL(request_tile_kernel, dim3((unsigned)((int64_t)t.tiles * t.parts + by_rows)), dim3(64 * kTileWaves), 0, st, t);
-    return hipGetLastError();
+    // Rows of a launch: a launch has fewer than 2^32 threads, and these are up to 2176 a row (r = 64).
+    constexpr int kRows = 1 << 20;
+    static_assert((64ll * kTileWaves * (kRows / 16 * 4 + (int64_t)kRows * (16 / kDownColumns) * 4 / kTileWaves)) < 1ll << 32, "threads of a launch");
+    for (int64_t row = 0; row < a.M; row += kRows) {
+        const int rows = (int)std::min<int64_t>(a.M - row, kRows);
+        const RequestTileArgs t{{a.X + row * a.K, a.A, a.ids + row, a.ranks, a.s, a.S + row * a.r, rows, a.K, a.r, a.P}, (rows + 15) / 16, a.r / 16};
+        const int64_t by_rows = ((int64_t)rows * (16 / kDownColumns) * t.parts + kTileWaves - 1) / kTileWaves;
+        hipLaunchKernelGGL(request_tile_kernel, dim3((unsigned)((int64_t)t.tiles * t.parts + by_rows)), dim3(64 * kTileWaves), 0, st, t);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_requests(const RequestArgs& a, hipStream_t st) {

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2510_00206_amd import binding
-from serve_util import BF16, F32, gen, normal, requests, within
+from serve_util import BF16, F32, U16, U32, gen, normal, requests, within
 
 pytestmark = pytest.mark.gpu
 
@@ -147,3 +147,32 @@ def test_first_product_by_rows_or_tiles(M, r):
     """Both sides of the line between single rows and tiles of rows in the first product."""
     for ids in ("one", "chunks", "any"):
         _check(_case(M, 704, 192, r, 6, ids, True, M + r), (M, r, ids))
+
+
+@pytest.mark.parametrize("M,r", [((1 << 21) - 1, 64), ((1 << 20) + 5, 16)])
+def test_most_rows(M, r):
+    """As many rows as the entry point takes, and a few more than one launch of the first product has."""
+    print("requests", M, r, flush=True)
+    K, N, P = 64, 64, 3
+    W, A, B = (t.cuda() for t in _case(1, K, N, r, P, "one", False, 9)[1:4])
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    X = torch.randn((M, K), generator=g, device="cuda").to(BF16)
+    ids = (torch.arange(M, device="cuda") // 37 % (P + 1) - 1).to(torch.int32)
+    ids[-70:] = torch.arange(70, device="cuda", dtype=torch.int32) % P
+    s = torch.tensor([0.5, -1.0, 2.0], device="cuda")
+    Y, S = torch.full((M, N), 7.0, dtype=BF16, device="cuda"), torch.full((M, r), 7.0, dtype=BF16, device="cuda")
+    binding.lora_requests_fwd(X, W, A, B, ids, s, Y=Y, S=S)
+    for rows in torch.arange(M, device="cuda").split(1 << 19):
+        x, of = X[rows].double(), ids[rows]
+        y, sums = x @ W.double().t(), x.abs() @ W.double().abs().t() * (K * U32)
+        t, tb = torch.zeros((rows.numel(), r), device="cuda", dtype=torch.float64), torch.zeros((rows.numel(), r), device="cuda", dtype=torch.float64)
+        for i in range(P):
+            at = of == i
+            a, b, sg = A[i].double(), B[i].double(), float(s[i])
+            t[at] = sg * (x[at] @ a.t())
+            tb[at] = U16 * t[at].abs() + abs(sg) * (K + 2) * U32 * (x[at].abs() @ a.abs().t())
+            y[at] += t[at] @ b.t()
+            sums[at] += tb[at] @ b.abs().t() + (r + 1) * U32 * (t[at].abs() @ b.abs().t())
+        assert bool(((S[rows].double() - t).abs() <= tb * (1 + U16)).all()), "S"
+        assert bool(((Y[rows].double() - y).abs() <= sums * (1 + U16) + U16 * y.abs()).all()), "Y"
