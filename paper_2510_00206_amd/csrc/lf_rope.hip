@@ -296,10 +296,22 @@ static hipError_t with_flags(bool a, bool b, F&& f) {
 hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st) {
     return with_lanes(a.D, [&](auto gl) {
         a.parts = rope_parts<gl()>(a.M, a.H, a.G, false);
-        const int64_t blocks = (a.M * a.parts + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
         return with_flags(interleaved, past_caches(a), [&](auto inter, auto past) {
-            hipLaunchKernelGGL((rope_fwd_kernel<gl(), inter(), past()>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
-            return hipGetLastError();
+            // (a launch has fewer than 2^32 threads: 64 a row)
+            constexpr int64_t ROWS = 1 << 25;
+            hipError_t e = hipSuccess;
+            for (int64_t left = a.M; left > 0 && e == hipSuccess; left -= ROWS) {
+                a.M = std::min(left, ROWS);
+                const int64_t blocks = (a.M * a.parts + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
+                hipLaunchKernelGGL((rope_fwd_kernel<gl(), inter(), past()>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
+                e = hipGetLastError();
+                a.q += a.M * a.ldq;
+                a.k += a.M * a.ldk;
+                a.q_out += a.M * a.ldqo;
+                a.k_out += a.M * a.ldko;
+                a.pos += a.M;
+            }
+            return e;
         });
     });
 }

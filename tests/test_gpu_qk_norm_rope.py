@@ -171,3 +171,17 @@ def test_rows_outside_the_tables_add_nothing(M, H, G, D, rot, inter):
         assert not got[i][out.cuda()].any()
         within(got[i][(~out).cuda()], dx, U16 * dx.abs() + (D + 32) * U32 * mag, ("dx", i))
         within(got[2 + i], dg, (D + 64 + 512) * U32 * mag_g, ("dgamma", i))
+
+
+def test_most_rows():
+    """As many rows as the entry points take; all hold one of 1000 rows, whose results the 64-bit form has."""
+    M, some, D = (1 << 26) - 1, 1000, 16
+    _, q, k, gq, gk, cos, sin, pos = (t.contiguous() for t in _inputs(some, 1, 1, D, 16, 8, packed=False))
+    at = torch.arange(M, device="cuda") % some
+    yq, yk = binding.lora_qk_norm_rope_fwd(*(t.cuda()[at] for t in (q, k)), gq.cuda(), gk.cuda(), cos.cuda(), sin.cuda(), pos.cuda()[at], eps=1e-5)
+    for y, x, gamma in ((yq, q, gq), (yk, k, gk)):
+        ref, bound = norm_rope(x.to(F64), gamma.to(F64), cos, sin, pos, 1e-5, False)
+        within(y[:some], ref, bound, "first rows")
+        for rows in y.split(some * 4000):
+            n = rows.shape[0] // some * some
+            assert bool((rows[:n].view(-1, some, D) == y[:some, 0]).all()) and torch.equal(rows[n:], y[:rows.shape[0] - n])
