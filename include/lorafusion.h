@@ -327,7 +327,8 @@ lora_status lora_qk_norm_rope_bwd(const lora_bf16* q, const lora_bf16* k, const 
 
 /* A paged cache of keys and values (the caller's device memory): k, v [pages, heads, page, dim].  fp8 == 0: lora_bf16.  fp8 != 0: e4m3
  * bytes, and k_exp, v_exp [pages, heads, page] with the biased exponent of one power of two for every token and head; the value is
- * e4m3 * 2^(exp - 127).  page: a power of two, 16 .. 1024 tokens; dim: multiples of 16 up to 256; heads up to 1024. */
+ * e4m3 * 2^(exp - 127).  page: a power of two, 16 .. 1024 tokens; dim: multiples of 16 up to 256; heads up to 1024.  Written and read: M * heads of 2^27 - 8
+ * and fewer. */
 typedef struct {
     void* k;
     void* v;

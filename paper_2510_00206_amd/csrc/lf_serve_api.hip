@@ -51,7 +51,8 @@ lora_status cache_copy(const lora_kv_cache* cache, const void* k, const void* v,
     if (!k || !v || !slots) return LORA_ERR_NULL;
     if (bad_stride(ldk, cache->heads, cache->dim) || bad_stride(ldv, cache->heads, cache->dim)) return LORA_ERR_SHAPE;
     if (misaligned(k) || misaligned(v) || misaligned(slots, 8)) return LORA_ERR_ALIGN;
-    if (M >= (1ll << 32) / (32ll * cache->heads)) return LORA_ERR_UNSUPPORTED;       // (32 lanes to a head at most; threads of a launch)
+    // (threads of a launch, in whole workgroups of 256; 32 lanes to a head at most)
+    if (M > ((1ll << 32) - 256) / (32ll * cache->heads)) return LORA_ERR_UNSUPPORTED;
     a.k = (lora_bf16*)k;
     a.v = (lora_bf16*)v;
     a.slots = slots;

@@ -133,3 +133,13 @@ def test_attention_workspace_serves_smaller_steps(lib):
         T1 = size(1, min(T, B1 * new1))
         large, small = (lib.lora_paged_attn_workspace_bytes(c, t, H, b, n, k, window) for t, b, n, k in ((T, B, new, kv), (T1, B1, new1, kv1)))
         assert 256 <= small <= large, (heads, dim, H, window, (T, B, new, kv), (T1, B1, new1, kv1))
+
+
+def test_cache_rows_of_a_launch(lib):
+    """Rows whose workgroups of 256 threads, 32 to a head, would pass the 2^32 threads of a launch are refused."""
+    p = P(0x1000)
+    for heads in (1, 3, 7, 8, 1000):
+        first = next(M for M in range((1 << 27) // heads - 20, (1 << 27) // heads + 20) if (M * heads * 32 + 255) // 256 * 256 >= 1 << 32)
+        c = _cache(dim=256, heads=heads)
+        assert lib.lora_kv_cache_write(c, p, p, 256 * heads, 256 * heads, p, first, None) == UNSUPPORTED, heads
+        assert lib.lora_kv_cache_read(c, p, first, p, p, 256 * heads, 256 * heads, None) == UNSUPPORTED, heads
