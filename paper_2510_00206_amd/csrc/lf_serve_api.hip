@@ -64,8 +64,8 @@ lora_status cache_copy(const lora_kv_cache* cache, const void* k, const void* v,
 
 lora_status check_attn(const PagedCache& c, int64_t T, int32_t H, int64_t B, int64_t max_new, int64_t max_kv, int32_t window) {
     if (T < 0 || B < 0 || H < 1 || max_new < 0 || max_kv < 0 || window < 0 || H % c.heads) return LORA_ERR_SHAPE;
-    if (!(c.D == 64 || c.D == 128) || T * H >= (1ll << 31) || max_new * H >= (1ll << 31) || max_kv >= (1ll << 30) || B >= (1ll << 31) ||
-        window >= (1 << 30))
+    const int64_t most = 0x7FFFFFFF / H;                   // (T * H could wrap)
+    if (!(c.D == 64 || c.D == 128) || T > most || max_new > most || max_kv >= (1ll << 30) || B >= (1ll << 31) || window >= (1 << 30))
         return LORA_ERR_UNSUPPORTED;
     return LORA_OK;
 }
@@ -175,7 +175,7 @@ lora_status lora_paged_attn_fwd(const lora_bf16* q, const lora_kv_cache* cache, 
     if (bad_stride(ldq, H, a.c.D) || bad_stride(ldo, H, a.c.D)) return LORA_ERR_SHAPE;
     if (misaligned(q) || misaligned(out) || misaligned(workspace, 256) || misaligned(table, 4) || misaligned(offsets, 4) || misaligned(kv_lens, 4))
         return LORA_ERR_ALIGN;
-    if (max_pages << a.c.page_shift >= 1ll << 30) return LORA_ERR_UNSUPPORTED;
+    if (max_pages >= 1ll << (30 - a.c.page_shift)) return LORA_ERR_UNSUPPORTED;
     const AttnPlan pl = plan_attn((int)B, a.c.heads, H / a.c.heads, a.c.D, (int)max_new, max_kv, window);
     if ((max_new * (H / a.c.heads) / pl.rows + 1) * pl.splits * B * a.c.heads >= 1ll << 24) return LORA_ERR_UNSUPPORTED;     // (threads of a launch)
     if (workspace_bytes < attn_scratch(pl, T, H, a.c.D)) return LORA_ERR_WORKSPACE;

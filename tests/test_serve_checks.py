@@ -143,3 +143,15 @@ def test_cache_rows_of_a_launch(lib):
         c = _cache(dim=256, heads=heads)
         assert lib.lora_kv_cache_write(c, p, p, 256 * heads, 256 * heads, p, first, None) == UNSUPPORTED, heads
         assert lib.lora_kv_cache_read(c, p, first, p, p, 256 * heads, 256 * heads, None) == UNSUPPORTED, heads
+
+
+def test_attention_sizes_that_wrap(lib):
+    """Sizes whose products pass 64 bits are refused as other large ones are."""
+    p, c = P(0x1000), _cache()
+    good = dict(q=p, cache=c, table=p, offsets=p, kv_lens=p, T=4, H=8, B=2, max_pages=5, ldq=512, ldt=5, ldo=512, max_new=2, max_kv=80, scale=0.1, window=0, out=p,
+                ws=p, n=1 << 30, stream=None)
+    for bad in (dict(T=1 << 61), dict(T=(1 << 61) + 4), dict(max_new=1 << 61), dict(max_new=(1 << 61) + 2), dict(max_pages=1 << 60, ldt=1 << 60),
+                dict(max_pages=(1 << 60) + 5, ldt=1 << 62)):
+        assert lib.lora_paged_attn_fwd(*_changed(good, **bad)) == UNSUPPORTED, bad
+    assert lib.lora_paged_attn_workspace_bytes(c, 1 << 61, 8, 2, 2, 80, 0) == 0
+    assert lib.lora_paged_attn_workspace_bytes(c, 4, 8, 2, 1 << 61, 80, 0) == 0
