@@ -339,7 +339,8 @@ typedef struct {
 } lora_kv_cache;
 
 /* Writes row i of k and v [M, heads, dim] to slot slots[i] = page number * page + place in it (device array; a slot outside the cache
- * is left out; slots of one call must differ, or one of the rows is kept, not always the same one).  fp8: the power of two is the
+ * is left out).  Slots of one call must differ: what a slot holds after two rows is undefined (keys of one beside values of the other, or
+ * its codes under the other's exponent); no other slot is affected.  fp8: the power of two is the
  * smallest (2^-117 at least, 1 for a head of zeros) that keeps the head's largest finite magnitude within 448; values are rounded to
  * nearest even, what is not finite becomes NaN. */
 lora_status lora_kv_cache_write(const lora_kv_cache* cache, const lora_bf16* k, const lora_bf16* v, int64_t ldk, int64_t ldv, const int64_t* slots,

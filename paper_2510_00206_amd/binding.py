@@ -474,7 +474,8 @@ class KVCache:
 
 
 def lora_kv_cache_write(cache: KVCache, k, v, slots):
-    """Rows of k, v [M, heads, dim] (rows may be apart) to the slots (int64: page number * page + place; outside the cache: left out)."""
+    """Rows of k, v [M, heads, dim] (rows may be apart) to the slots (int64: page number * page + place; outside the cache: left out; each at most
+    once)."""
     M = slots.numel()
     assert k.shape == (M, cache.heads, cache.dim) and v.shape == k.shape, "shapes do not fit"
     kp, ldk = _heads(k)

@@ -150,3 +150,20 @@ def test_large_reads(M, G, D, fp8):
         if not fp8:
             kv[5] = 0
             assert torch.equal(whole[i], kv[:, i])
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_a_slot_that_two_rows_name(fp8):
+    """Undefined in itself, and without effect on any other slot."""
+    cache = binding.KVCache.empty(4, 16, 3, 128, fp8)
+    x = normal(gen(4), (40, 3, 128))
+    slots = torch.arange(40) + 10
+    slots[20:30] = 12
+    binding.lora_kv_cache_write(cache, x.cuda(), (-x).cuda(), slots.cuda())
+    single = torch.tensor([i for i in range(40) if slots[i] != 12])
+    k, v = binding.lora_kv_cache_read(cache, slots[single].cuda())
+    want = widened(*quantised(x[single])) if fp8 else x[single].double()
+    assert torch.equal(k.cpu().double(), want) and torch.equal(v.cpu().double(), -want)
+    others = torch.tensor([i for i in range(64) if i not in slots.tolist()])
+    k, v = binding.lora_kv_cache_read(cache, others.cuda())
+    assert not k.any() and not v.any()
