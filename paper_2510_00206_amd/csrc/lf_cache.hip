@@ -3,7 +3,7 @@
 // three fraction bits, and what is read back (value x scale) is exact in bf16.  Bound by HBM: 3 + 1 / D bytes an element (bf16: 4).  Eight
 // entries to a lane, a head to 8, 16 or 32 lanes, whose largest magnitude comes from the bit patterns (integers in the order of the values).
 // Measured: 2085 tokens of 8 heads of 128 to fp8, 13 MB, 5.5 us (slot, then the head: two latencies), 32768 tokens, 203 MB, 56 us; 29999 tokens read back from
-// fp8, 185 MB, 32 us.  Read with two or four heads to a lane, all their loads under way, and ordinary stores 48 us, with one 44.
+// fp8, 185 MB, 44 us; with two or four heads to a lane, all their loads under way, 48.
 #include "lf_serve.h"
 
 namespace lf {
@@ -87,7 +87,9 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheCopyArgs p) {
             out = *(const u32x4*)((const lora_bf16*)(keys ? p.c.k : p.c.v) + at * p.c.D + 8 * j);
         }
     }
-    put8<PAST>((keys ? p.k + t * p.ldk : p.v + t * p.ldv) + (int64_t)head * p.c.D + 8 * j, out);
+    u32x4* to = (u32x4*)((keys ? p.k + t * p.ldk : p.v + t * p.ldv) + (int64_t)head * p.c.D + 8 * j);
+    if constexpr (PAST) __builtin_nontemporal_store(out, to);
+    else *to = out;
 }
 
 template <class F>
@@ -105,13 +107,14 @@ hipError_t launch_cache_write(const CacheCopyArgs& a, hipStream_t st) {
     });
 }
 
-// Outputs of 64 MB and more go past the caches: ordinary stores leave them in the L2s, to be written back when the kernel ends.  us, stored / past the caches, by
-// itself and with the reading of the outputs by another kernel behind it: 29999 tokens of 8 heads of 128, fp8 (123 MB) 44.5 / 31.5, 79.8 / 75.8; 8000 (33 MB)
-// 22.0 / 23.7 with it.
+// Outputs of 176 MB and more, which the 256 MB memory-side cache does not hold beside what is read, go past the caches.  us, stored / past the caches, alone
+// and with the reading of the outputs by another kernel behind, three sets in turn, fp8, 8 heads of 128: 16000 tokens (66 MB) 25.7 / 18.4, 48.3 / 51.7; 29999
+// (123 MB) 44.6 / 30.6, 85 / 89; 36000 53.4 / 36.6, 104.5 / 105.3; 48000 (197 MB) 69.6 / 65.8, 139.5 / 135.8; 72000 104.1 / 96.4, 206.2 / 199.6; bf16, 16000
+// 26.2 / 21.0, 48.6 / 53.5; from 48000 on level with the reader.
 hipError_t launch_cache_read(const CacheCopyArgs& a, hipStream_t st) {
     return with_lanes(a, [&](auto gl) {
         const int64_t blocks = (a.M * a.c.heads * gl() + 255) / 256;
-        if (a.M * a.c.heads * a.c.D * 4 >= 64 << 20) hipLaunchKernelGGL((cache_read_kernel<gl(), true>), dim3((unsigned)blocks, 2), dim3(256), 0, st, a);
+        if (a.M * a.c.heads * a.c.D * 4 >= 176 << 20) hipLaunchKernelGGL((cache_read_kernel<gl(), true>), dim3((unsigned)blocks, 2), dim3(256), 0, st, a);
         else hipLaunchKernelGGL((cache_read_kernel<gl(), false>), dim3((unsigned)blocks, 2), dim3(256), 0, st, a);
         return hipGetLastError();
     });

@@ -5,8 +5,11 @@
 // fp32, the result is rounded once.  Bound by HBM: 4 (6) bytes an element.  Eight entries to a lane (16-byte loads), 8, 16 or
 // 32 lanes to a head by its size; a head's sums are butterflies over its lanes.  With R's cosines and sines multiplied by gamma once per
 // row, y is one product and one multiply-add an entry; a pair's other entry comes from the lane that holds it, as the bf16 it was.
-// Measured (a copy of 2 GiB runs at 4.9 TB/s): forward, 8192 rows of 32 + 8 heads of 128, 168 MB, 34 us, 4.9 TB/s; backward, 5003 rows of 64 + 8, 277 MB, 53 us,
-// 5.2 TB/s, and 4.7 us for the sum of its planes; forward of 16 rows 4 us: the launch, and position, table and row read one after the other.
+// Outputs are ordinary stores.  Past the caches the kernels themselves are faster, their reader is slower by more: us, stored / past the caches, alone and with
+// the reading of the outputs behind, three sets in turn, 32 + 8 heads of 128: forward, 2048 rows (21 MB) 12.7 / 11.1, 21.4 / 21.5; 8192 (84 MB) 39.3 / 34.3, 69.5 / 71.6;
+// 32768 (336 MB) 130.6 / 122.9, 241.7 / 252.4; backward, 4096 rows 34.8 / 30.8, 53.8 / 55.4; 8192 58.2 / 55.3, 95.5 / 94.7; 16384 105.4 / 99.5, 173.0 / 180.8.
+// Measured (a copy of 2 GiB runs at 4.9 TB/s): forward, 8192 rows of 32 + 8 heads of 128, 168 MB, 38.7 us, 4.3 TB/s; backward, 5003 rows of 64 + 8, 277 MB, 61 us,
+// 4.7 of them the sum of its planes; forward of 16 rows 4 us: the launch, and position, table and row read one after the other.
 #include <algorithm>
 
 #include "lf_serve.h"
@@ -95,7 +98,7 @@ struct RopePasses {
     __host__ __device__ RopePasses(int H, int G) : of_q((H + HEADS - 1) / HEADS), all((H + HEADS - 1) / HEADS + (G + HEADS - 1) / HEADS) {}
 };
 
-template <int GL, bool INTER, bool PAST>
+template <int GL, bool INTER>
 __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
     const int64_t unit = (int64_t)blockIdx.x * (kRopeThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = unit / p.parts;
@@ -144,7 +147,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
                 for (int i = 0; i < 8; ++i) y[i] = inv * (x[i] * cg[i] + o[i] * sg[i]);
                 u32x4 out = pack8(y);
                 if (!known) out = u32x4{0u, 0u, 0u, 0u};
-                if (ok[u]) put8<PAST>(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j, out);
+                if (ok[u]) *(u32x4*)(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j) = out;
             }
         }
     };
@@ -153,7 +156,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
     heads(p.k + row * p.ldk, p.k_out + row * p.ldko, p.G, ps.all - ps.of_q, ps.first_k(part, p.parts), ck, sk);
 }
 
-template <int GL, bool INTER, bool PAST>
+template <int GL, bool INTER>
 __global__ void __launch_bounds__(64 * rope_bwd_waves(GL), rope_bwd_waves(GL)) rope_bwd_kernel(RopeArgs p) {
     constexpr int WAVES = rope_bwd_waves(GL);
     __shared__ float red[WAVES][2][GL * 8];
@@ -214,7 +217,7 @@ __global__ void __launch_bounds__(64 * rope_bwd_waves(GL), rope_bwd_waves(GL)) r
                     }
                     u32x4 out = pack8(dx);
                     if (!known) out = u32x4{0u, 0u, 0u, 0u};
-                    if (ok[u]) put8<PAST>(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j, out);
+                    if (ok[u]) *(u32x4*)(out_row + (int64_t)(pass * ps.HEADS + ln.slot) * p.D + 8 * ln.j) = out;
                 }
             }
         };
@@ -276,10 +279,6 @@ static int rope_parts(int64_t M, int H, int G, bool backward) {
     const int64_t want = std::max((16 * kComputeUnits + M - 1) / std::max<int64_t>(M, 1), (int64_t)(backward ? (all + 2) / 4 | 1 : 1));
     return (int)std::min<int64_t>(want, all);
 }
-// Outputs of 16 MB and more go past the caches: ordinary stores leave them in the L2s, to be written back when the kernel ends.  us, stored / past the caches,
-// 32 + 8 heads of 128, by itself and with the reading of the outputs by another kernel behind it: 64 rows (0.7 MB) 9.6 / 9.6, 7.4 / 7.7; 512 (5 MB) 10.1 / 10.1
-// with it; 2048 (21 MB) 13.4 / 12.0, 22.1 / 21.5; 8192 (84 MB) 39.6 / 34.0, 58.5 / 59.7; backward, 8192 57.7 / 54.4.
-static bool past_caches(const RopeArgs& a) { return a.M * (a.H + a.G) * a.D * 2 >= 16 << 20; }
 template <class F>
 static auto with_lanes(int D, F&& f) {
     if (D <= 64) return f(std::integral_constant<int, 8>{});
@@ -288,22 +287,19 @@ static auto with_lanes(int D, F&& f) {
 }
 
 template <class F>
-static hipError_t with_flags(bool a, bool b, F&& f) {
-    if (a) return b ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
-    return b ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
-}
+static hipError_t with_pairs(bool interleaved, F&& f) { return interleaved ? f(std::true_type{}) : f(std::false_type{}); }
 
 hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st) {
     return with_lanes(a.D, [&](auto gl) {
         a.parts = rope_parts<gl()>(a.M, a.H, a.G, false);
-        return with_flags(interleaved, past_caches(a), [&](auto inter, auto past) {
+        return with_pairs(interleaved, [&](auto inter) {
             // (a launch has fewer than 2^32 threads: 64 a row)
             constexpr int64_t ROWS = 1 << 25;
             hipError_t e = hipSuccess;
             for (int64_t left = a.M; left > 0 && e == hipSuccess; left -= ROWS) {
                 a.M = std::min(left, ROWS);
                 const int64_t blocks = (a.M * a.parts + kRopeThreads / 64 - 1) / (kRopeThreads / 64);
-                hipLaunchKernelGGL((rope_fwd_kernel<gl(), inter(), past()>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
+                hipLaunchKernelGGL((rope_fwd_kernel<gl(), inter()>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
                 e = hipGetLastError();
                 a.q += a.M * a.ldq;
                 a.k += a.M * a.ldk;
@@ -327,8 +323,8 @@ hipError_t launch_rope_bwd(RopeArgs a, bool interleaved, const RopeFinalizeArgs&
     if (f.blocks > 0) {
         const hipError_t e = with_lanes(a.D, [&](auto gl) {
             a.parts = rope_parts<gl()>(a.M, a.H, a.G, true);
-            return with_flags(interleaved, past_caches(a), [&](auto inter, auto past) {
-                hipLaunchKernelGGL((rope_bwd_kernel<gl(), inter(), past()>), dim3(f.blocks), dim3(64 * rope_bwd_waves(gl())), 0, st, a);
+            return with_pairs(interleaved, [&](auto inter) {
+                hipLaunchKernelGGL((rope_bwd_kernel<gl(), inter()>), dim3(f.blocks), dim3(64 * rope_bwd_waves(gl())), 0, st, a);
                 return hipGetLastError();
             });
         });

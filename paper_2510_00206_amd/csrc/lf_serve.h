@@ -76,12 +76,6 @@ __device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
     return u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
 }
 
-template <bool PAST>
-__device__ __forceinline__ void put8(lora_bf16* to, u32x4 v) {      // PAST: past the caches
-    if constexpr (PAST) __builtin_nontemporal_store(v, (u32x4*)to);
-    else *(u32x4*)to = v;
-}
-
 // Maximum (sum) over the four lanes of a wave that share l & 15.
 template <class F>
 __device__ __forceinline__ float over_quarters(float x, F&& f) {

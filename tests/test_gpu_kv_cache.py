@@ -167,3 +167,24 @@ def test_a_slot_that_two_rows_name(fp8):
     others = torch.tensor([i for i in range(64) if i not in slots.tolist()])
     k, v = binding.lora_kv_cache_read(cache, others.cuda())
     assert not k.any() and not v.any()
+
+
+@pytest.mark.parametrize("M,G,D,fp8", [(46000, 8, 128, True), (46001, 8, 128, False), (92000, 8, 64, True), (23003, 8, 256, True), (185000, 2, 80, False)])
+def test_larger_reads(M, G, D, fp8):
+    """Outputs on both sides of the size from which they go past the caches."""
+    page = 16
+    cache = binding.KVCache.empty(M // page + 1, page, G, D, fp8)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M)
+    kv = torch.randn((M, 2, G, D), generator=g, device="cuda").to(BF16)
+    slots = torch.randperm(M // page * page + page, generator=g, device="cuda")[:M]
+    binding.lora_kv_cache_write(cache, kv[:, 0], kv[:, 1], slots)
+    slots[77] = -1
+    whole = binding.lora_kv_cache_read(cache, slots)
+    assert 4 * whole[0].numel() >= 176 << 20 or D == 80
+    pieces = [binding.lora_kv_cache_read(cache, part.contiguous()) for part in slots.split(4001)]
+    for i in range(2):
+        assert torch.equal(whole[i], torch.cat([p[i] for p in pieces])) and not whole[i][77].any()
+        if not fp8:
+            kv[77] = 0
+            assert torch.equal(whole[i], kv[:, i])
