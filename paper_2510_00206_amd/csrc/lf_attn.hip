@@ -1031,12 +1031,9 @@ AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, 
 
 template <auto KERNEL>
 static hipError_t launch_lds(int lds, unsigned blocks, const AttnArgs& a, hipStream_t st) {
-    static bool attr_set = false;                  // one flag per kernel
-    if (!attr_set) {
-        const hipError_t e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
+    static std::atomic<uint64_t> allowed{0};       // one per kernel
+    const hipError_t e = allow_lds((const void*)KERNEL, lds, allowed);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(KERNEL, dim3(blocks), dim3(256), lds, st, a);
     return hipGetLastError();
 }

@@ -867,12 +867,9 @@ template <class C>
 static hipError_t launch_requests_cfg(const RingRequestArgs& a, hipStream_t st) {
     constexpr int LDS = C::LDS + C::NW * (int)sizeof(RequestList<C>);
     static_assert(LDS <= 160 * 1024, "a compute unit's LDS");
-    static bool attr_set = false;                  // one flag per instantiation
-    if (!attr_set) {
-        hipError_t e = hipFuncSetAttribute((const void*)ring_requests_kernel<C>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
+    static std::atomic<uint64_t> allowed{0};       // one per instantiation
+    const hipError_t e = allow_lds((const void*)ring_requests_kernel<C>, LDS, allowed);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(ring_requests_kernel<C>, dim3((unsigned)((int64_t)a.tiles_m * a.tiles_n)), dim3(C::THREADS + 64 * C::CW), LDS, st, a);
     return hipGetLastError();
 }

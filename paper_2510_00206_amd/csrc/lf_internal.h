@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stddef.h>
+#include <atomic>
 #include <type_traits>
 #include <string.h>
 
@@ -11,6 +12,18 @@
 typedef uint16_t lora_bf16;
 
 namespace lf {
+
+// Dynamic LDS of a kernel, which has to be allowed once on every device.  `allowed`: one to a kernel, a bit to a device; launches may come from several threads.
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& allowed) {
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0ull;
+    if (allowed.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 // Operation (1): S' = s*q*(mask.X) A^T.
 template <class TB>

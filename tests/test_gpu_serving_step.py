@@ -1,5 +1,7 @@
 """The operators around served adapters together, as examples/serving_step.py runs them: chunks and decoding against the whole prompt in 64 bits,
 replays of a captured step against eager ones, a stream of its own, and the training step's gradients."""
+import threading
+
 import torch
 import pytest
 
@@ -123,6 +125,33 @@ def test_a_stream_of_its_own():
             out.append(block.serve(step, x).clone())
     torch.cuda.synchronize()
     assert torch.equal(out[0], out[1])
+
+
+def test_steps_from_several_threads():
+    """Four threads, each with a stream, a cache and a step of its own size, at the same time: as one after the other."""
+    block = _block()
+    sizes = [[40], [1, 1, 1], [70, 2], [12]]
+    x = [torch.randn((sum(n), 320), device="cuda").to(BF16) for n in sizes]
+
+    def run(i, out, stream):
+        with torch.cuda.stream(stream):
+            for k in range(20):
+                cache = binding.KVCache.empty(20, 16, block.kv_heads, block.dim, bool(i % 2))
+                step = Step(block, cache, sizes[i], 80, 6)
+                step.plan([2] * len(sizes[i]), [[6 * b + j for j in range(6)] for b in range(len(sizes[i]))], [0] * len(sizes[i]))
+                out[i] = block.serve(step, x[i]).clone()
+            stream.synchronize()
+    streams = [torch.cuda.Stream() for _ in sizes]
+    torch.cuda.synchronize()
+    together, alone = [None] * 4, [None] * 4
+    threads = [threading.Thread(target=run, args=(i, together, streams[i])) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i in range(4):
+        run(i, alone, streams[i])
+    assert all(torch.equal(a, b) for a, b in zip(together, alone))
 
 
 def test_training_step():
