@@ -339,7 +339,6 @@ struct RequestTerm {
         int of = p.ids[rt.row_start + min(row, rt.rows - 1)];
         if (l >= ROWS || row >= rt.rows || of >= p.P || of < 0) of = -1;
         const int rank = of < 0 ? 0 : p.ranks ? max(min(p.ranks[of], p.lr), 0) : p.lr;
-        if (l < ROWS) out.id[l] = of;
         // the rows of each row's adapter, from the bits of their numbers; the first of them enters it
         uint64_t its = __ballot(rank > 0);
         if (!its) return;
