@@ -127,6 +127,37 @@ def test_a_stream_of_its_own():
     assert torch.equal(out[0], out[1])
 
 
+def test_a_busy_stream():
+    """All calls of a step wait for the work that its stream still has before them: launched anywhere else they would read zeros."""
+    block = _block()
+    x = torch.randn((40, 320), device="cuda").to(BF16)
+    big = torch.randn((8192, 8192), device="cuda").to(BF16)
+    out, spare = [], torch.empty_like(big)
+    stream = torch.cuda.Stream()
+    for busy in (False, True):
+        cache = binding.KVCache.empty(3, 16, block.kv_heads, block.dim, True)
+        step = Step(block, cache, [40], 40, 3)
+        late, positions, adapters = torch.zeros_like(x), torch.zeros_like(step.positions), torch.zeros_like(step.adapters)
+        step.plan([2], [[0, 1, 2]], [0])
+        for mine, right in ((positions, "positions"), (adapters, "adapters")):
+            mine.copy_(getattr(step, right))
+            getattr(step, right).zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            ready = torch.cuda.Event()
+            for _ in range(200 if busy else 0):             # some 170 ms, which the launches below take less than
+                torch.mm(big, big, out=spare)
+            late.copy_(x)
+            step.positions.copy_(positions)
+            step.adapters.copy_(adapters)
+            ready.record()
+            out.append(block.serve(step, late).clone())
+            early = not ready.query()
+        torch.cuda.synchronize()
+        assert early or not busy, "the stream's work ended before the step was launched"
+    assert torch.equal(out[0], out[1])
+
+
 def test_steps_from_several_threads():
     """Four threads, each with a stream, a cache and a step of its own size, at the same time: as one after the other."""
     block = _block()
