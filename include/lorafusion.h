@@ -291,14 +291,16 @@ lora_status lora_ceiling_hbm_read(const void* src, size_t bytes, uint32_t* sink,
  * Once trained, adapters are served: a step holds the rows of many requests, each with its own adapter, then the attention of
  * their new tokens over a cache of keys and values.  The same conventions as above; "device arrays" are read by the kernels, so their
  * values are not checked on the host, and what is out of range in them is handled as each call says.  Strides (ld*) are the
- * distances of rows in elements, multiples of 8, the heads of a row lying side by side.  fp32 inside; outputs rounded once. */
+ * distances of rows in elements, multiples of 8, the heads of a row lying side by side.  Sums, norms and the softmax are fp32 and outputs are
+ * rounded once; what stands between two products is rounded to bf16 before the second: S of lora_requests_fwd and the weights of
+ * lora_paged_attn_fwd. */
 
 /* Forward of a batch in which every row names its adapter:
  *   Y[i] = X[i] W^T + s[g] (X[i] A[g]^T) B[g]^T,   g = ids[i];  a row with ids[i] outside 0 .. P-1 has no adapter.
  * X [M,K]  W [N,K]  A [P,r,K]  B [P,N,r]  Y [M,N];  device arrays ids [M], s [P], ranks [P].  ranks (may be NULL: all r): adapter g
  * uses the first ranks[g] rows of A[g] and columns of B[g], any number of 0 .. r (values outside are cut to it); the others may
- * hold anything.  S [M,r]: scratch that receives s (X A^T), zero past the rank.  No dropout: a row's result is that of lora_fwd
- * with p = 0 up to the order of the sums in S.  M < 2^21, K, N, r as above; any P >= 1; adapters may come in any order and number. */
+ * hold anything.  S [M,r]: scratch that receives s (X A^T) in bf16, as the second product takes it, zero past the rank.  No dropout: a
+ * row's result is that of lora_fwd with p = 0 up to the order of the sums in S and Y.  M < 2^21, K, N, r as above; any P >= 1; adapters may come in any order and number. */
 lora_status lora_requests_fwd(const lora_bf16* X, const lora_bf16* W, const lora_bf16* A, const lora_bf16* B, const int32_t* ids,
                               const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P, lora_bf16* Y,
                               lora_bf16* S, lora_stream stream);
@@ -327,8 +329,8 @@ lora_status lora_qk_norm_rope_bwd(const lora_bf16* q, const lora_bf16* k, const 
 
 /* A paged cache of keys and values (the caller's device memory): k, v [pages, heads, page, dim].  fp8 == 0: lora_bf16.  fp8 != 0: e4m3
  * bytes, and k_exp, v_exp [pages, heads, page] with the biased exponent of one power of two for every token and head; the value is
- * e4m3 * 2^(exp - 127).  page: a power of two, 16 .. 1024 tokens; dim: multiples of 16 up to 256; heads up to 1024.  Written and read: M * heads of 2^27 - 8
- * and fewer. */
+ * e4m3 * 2^(exp - 127), exp 10 .. 247 (what a write gives), or less beside codes of zero (a cache cleared to zeros).  page: a power of
+ * two, 16 .. 1024 tokens; dim: multiples of 16 up to 256; heads up to 1024.  Written and read: M * heads of 2^27 - 8 and fewer. */
 typedef struct {
     void* k;
     void* v;
@@ -340,9 +342,9 @@ typedef struct {
 
 /* Writes row i of k and v [M, heads, dim] to slot slots[i] = page number * page + place in it (device array; a slot outside the cache
  * is left out).  Slots of one call must differ: what a slot holds after two rows is undefined (keys of one beside values of the other, or
- * its codes under the other's exponent); no other slot is affected.  fp8: the power of two is the
- * smallest (2^-117 at least, 1 for a head of zeros) that keeps the head's largest finite magnitude within 448; values are rounded to
- * nearest even, what is not finite becomes NaN. */
+ * its codes under the other's exponent); no other slot is affected.  fp8: the power of two is the smallest (2^-117 at least, 1 for a head
+ * of zeros) that keeps the head's largest finite magnitude within 448; values are rounded to nearest even (from 1.9375 * 2^127 on to 2^128,
+ * which reads as infinity), what is not finite becomes NaN. */
 lora_status lora_kv_cache_write(const lora_kv_cache* cache, const lora_bf16* k, const lora_bf16* v, int64_t ldk, int64_t ldv, const int64_t* slots,
                                 int64_t M, lora_stream stream);
 /* ... and reads slots back, exactly; a slot outside the cache reads as zeros. */
@@ -354,13 +356,15 @@ lora_status lora_kv_cache_read(const lora_kv_cache* cache, const int64_t* slots,
  * is row j % page of page table[b * ldt + j / page].  The new token at position pos sees the keys j <= pos and, with window > 0, only
  * j > pos - window; query head h uses key/value head h / (H / heads).
  *   out = sum_j softmax_j(scale q k_j) v_j;   a row that sees no key (fewer keys than new tokens): zeros.
+ * The weights are rounded to bf16 after their exponential and divided by the sum of the rounded ones, so that equal values come back as they are.
  * offsets [B+1], kv_lens [B] and table are device arrays; max_new and max_kv (host) are the largest number of new tokens and the largest
  * length: rows past max_new of a sequence are not computed, and a larger length than max_kv costs time only.  Lengths are cut to max_pages
  * pages and page numbers to the cache.  Cache entries past a sequence's length, and keys that a row does not see, may hold anything.
  * dim 64 or 128; T * H < 2^31; lengths below 2^30; q k_j and scale q k_j up to 2^126 in magnitude.  workspace: device scratch of at
- * least lora_paged_attn_workspace_bytes(), 256-byte aligned, which is enough for every call with this H, window and form of cache whose T, B, max_new and max_kv
- * are at most these (fewer rows are cut into more parts, so that a smaller step may use more of it).  The same inputs and sizes give the same
- * bits. */
+ * least lora_paged_attn_workspace_bytes(), 256-byte aligned, which is enough for every call with this H, window and form of cache whose T,
+ * B, max_new and max_kv are at most these (fewer rows are cut into more parts, so that a smaller step may use more of it).  A chunk beside
+ * decoding sequences is faster as two calls: the longest chunk decides how all sequences of a call are taken.  The same inputs and sizes
+ * give the same bits. */
 size_t lora_paged_attn_workspace_bytes(const lora_kv_cache* cache, int64_t T, int32_t H, int64_t B, int64_t max_new, int64_t max_kv, int32_t window);
 lora_status lora_paged_attn_fwd(const lora_bf16* q, const lora_kv_cache* cache, const int32_t* table, const int32_t* offsets, const int32_t* kv_lens,
                                 int64_t T, int32_t H, int64_t B, int64_t max_pages, int64_t ldq, int64_t ldt, int64_t ldo, int64_t max_new,
