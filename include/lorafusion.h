@@ -362,9 +362,9 @@ lora_status lora_kv_cache_read(const lora_kv_cache* cache, const int64_t* slots,
  * pages and page numbers to the cache.  Cache entries past a sequence's length, and keys that a row does not see, may hold anything.
  * dim 64 or 128; T * H < 2^31; lengths below 2^30; q k_j and scale q k_j up to 2^126 in magnitude.  workspace: device scratch of at
  * least lora_paged_attn_workspace_bytes(), 256-byte aligned, which is enough for every call with this H, window and form of cache whose T,
- * B, max_new and max_kv are at most these (fewer rows are cut into more parts, so that a smaller step may use more of it).  A chunk beside
- * decoding sequences is faster as two calls: the longest chunk decides how all sequences of a call are taken.  The same inputs and sizes
- * give the same bits. */
+ * B, max_new and max_kv are at most these (fewer rows are cut into more parts, so that a smaller step may use more of it; never more than
+ * 2^18 rows of dim + 2 floats, where T is within B * max_new).  Chunks beside decoding sequences of long caches are faster as two calls: the
+ * longest chunk decides how all sequences of a call are taken.  The same inputs and sizes give the same bits. */
 size_t lora_paged_attn_workspace_bytes(const lora_kv_cache* cache, int64_t T, int32_t H, int64_t B, int64_t max_new, int64_t max_kv, int32_t window);
 lora_status lora_paged_attn_fwd(const lora_bf16* q, const lora_kv_cache* cache, const int32_t* table, const int32_t* offsets, const int32_t* kv_lens,
                                 int64_t T, int32_t H, int64_t B, int64_t max_pages, int64_t ldq, int64_t ldt, int64_t ldo, int64_t max_new,
