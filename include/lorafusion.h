@@ -327,10 +327,29 @@ lora_status lora_qk_norm_rope_bwd(const lora_bf16* q, const lora_bf16* k, const 
                                   lora_bf16* dk, float* dgamma_q, float* dgamma_k, int accumulate, void* workspace, size_t workspace_bytes,
                                   lora_stream stream);
 
-/* A paged cache of keys and values (the caller's device memory): k, v [pages, heads, page, dim].  fp8 == 0: lora_bf16.  fp8 != 0: e4m3
+/* 4 bits, of weights and of the cache: e2m1 codes (bit 3 the sign, the others 0, 0.5, 1, 1.5, 2, 3, 4, 6 in this order), two to a byte, the first in its low
+ * half, and for 32 entries in a row the biased exponent of one power of two, a byte; the value is e2m1 * 2^(exp - 127), which bf16 holds exactly.
+ * Written, the power of two is the smallest (2^-125 at least, 1 for 32 zeros; exp 2 .. 253) that keeps the largest magnitude within 6; values are rounded to
+ * nearest even (from 3.5 * 2^126 on to 2^128, which reads as infinity).  32 entries with one that is not finite are held as NaN, all of them: exp 255.  Exponents below 2 are
+ * read where their values are zeros (what is cleared to zeros reads as zeros).
+ *
+ * Weights W [N,K] into that form, codes [N, K/2] and exps [N, K/32] (device bytes, 16-byte aligned), and back, exactly: what the training entry points take of
+ * frozen weights that are held in 4 bits.  K and N: positive multiples of 64 up to 2^22. */
+lora_status lora_weights_write(const lora_bf16* W, int64_t N, int64_t K, uint8_t* codes, uint8_t* exps, lora_stream stream);
+lora_status lora_weights_read(const uint8_t* codes, const uint8_t* exps, int64_t N, int64_t K, lora_bf16* W, lora_stream stream);
+
+/* lora_requests_fwd over such weights, without a copy of them in bf16: the arguments are its own, with codes and exps for W.  P = 0: no adapters (A, B, ids, ranks, s, S
+ * may be NULL, r anything). */
+lora_status lora_requests_quantised_fwd(const lora_bf16* X, const uint8_t* codes, const uint8_t* exps, const lora_bf16* A, const lora_bf16* B,
+                                        const int32_t* ids, const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P,
+                                        lora_bf16* Y, lora_bf16* S, lora_stream stream);
+
+/* A paged cache of keys and values (the caller's device memory): k, v [pages, heads, page, dim].  fp8 == 0: lora_bf16.  fp8 == LORA_KV_FP4: 4 bits, k, v
+ * [pages, heads, page, dim/2] bytes, k_exp, v_exp [pages, heads, page, dim/32], dim a multiple of 32.  Any other fp8: e4m3
  * bytes, and k_exp, v_exp [pages, heads, page] with the biased exponent of one power of two for every token and head; the value is
  * e4m3 * 2^(exp - 127), exp 10 .. 247 (what a write gives), or less beside codes of zero (a cache cleared to zeros).  page: a power of
  * two, 16 .. 1024 tokens; dim: multiples of 16 up to 256; heads up to 1024.  Written and read: M * heads of 2^27 - 8 and fewer. */
+#define LORA_KV_FP4 (-4)
 typedef struct {
     void* k;
     void* v;
@@ -347,9 +366,18 @@ typedef struct {
  * which reads as infinity), what is not finite becomes NaN. */
 lora_status lora_kv_cache_write(const lora_kv_cache* cache, const lora_bf16* k, const lora_bf16* v, int64_t ldk, int64_t ldv, const int64_t* slots,
                                 int64_t M, lora_stream stream);
-/* ... and reads slots back, exactly; a slot outside the cache reads as zeros. */
+/* (4 bits: above.)  ... and reads slots back, exactly; a slot outside the cache reads as zeros. */
 lora_status lora_kv_cache_read(const lora_kv_cache* cache, const int64_t* slots, int64_t M, lora_bf16* k, lora_bf16* v, int64_t ldk, int64_t ldv,
                                lora_stream stream);
+
+/* lora_qk_norm_rope_fwd and lora_kv_cache_write in one pass: the normalised and turned queries go to q_out [M,H,dim], the keys and v [M,heads,dim] to their slots.
+ * gamma_q and gamma_k NULL (both): no norm, the rotation alone; eps is checked all the same.  Keys that the cache holds in fewer bits are formed in 64 bits and rounded
+ * once, to its codes (magnitudes from 2^128 on count as not finite); everything else is as in those two calls, a row outside the tables: zeros for query
+ * and keys, a slot outside the cache: left out.  q_out may be q.  dim, rot, H and M as in the first. */
+lora_status lora_kv_cache_append(const lora_kv_cache* cache, const lora_bf16* q, const lora_bf16* k, const lora_bf16* v, const lora_bf16* gamma_q,
+                                 const lora_bf16* gamma_k, const float* cos_table, const float* sin_table, const int32_t* pos, const int64_t* slots, int64_t M,
+                                 int32_t H, int32_t rot, int64_t positions, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, float eps, int interleaved,
+                                 lora_bf16* q_out, lora_stream stream);
 
 /* Attention of new tokens over a paged cache that holds them already.  q, out [T, H, dim]: the new tokens of B sequences end to end,
  * sequence b's being rows offsets[b] .. offsets[b+1]-1; with kv_lens[b] tokens in the cache, the last of them the new ones; its token j

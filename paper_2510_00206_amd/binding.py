@@ -22,7 +22,8 @@ EXPORTS = ("lora_fwd", "lora_bwd", "lora_bwd_noalloc", "multi_lora_fwd", "multi_
            "lora_debug_da_panels", "lora_debug_bwd_plan", "lora_debug_gemm_tiles", "lora_debug_launches",
            "lora_unfused_fwd", "lora_unfused_bwd", "lora_unfused_workspace_bytes",
            "lora_requests_fwd", "lora_qk_norm_rope_fwd", "lora_qk_norm_rope_bwd", "lora_qk_norm_rope_workspace_bytes",
-           "lora_kv_cache_write", "lora_kv_cache_read", "lora_paged_attn_fwd", "lora_paged_attn_workspace_bytes")
+           "lora_kv_cache_write", "lora_kv_cache_read", "lora_paged_attn_fwd", "lora_paged_attn_workspace_bytes",
+           "lora_weights_write", "lora_weights_read", "lora_requests_quantised_fwd", "lora_kv_cache_append")
 
 _lib = None
 
@@ -111,12 +112,16 @@ def load_library() -> C.CDLL:
     lib.lora_qk_norm_rope_workspace_bytes.argtypes = [I64, I32, I32, I32]
     lib.lora_kv_cache_write.argtypes = [CA, P, P, I64, I64, P, I64, P]
     lib.lora_kv_cache_read.argtypes = [CA, P, I64, P, P, I64, I64, P]
+    lib.lora_weights_write.argtypes = [P, I64, I64, P, P, P]
+    lib.lora_weights_read.argtypes = [P, P, I64, I64, P, P]
+    lib.lora_requests_quantised_fwd.argtypes = [P] * 8 + [I64, I64, I64, I32, I64, P, P, P]
+    lib.lora_kv_cache_append.argtypes = [CA] + [P] * 9 + [I64, I32, I32, I64, I64, I64, I64, I64, F, C.c_int, P, P]
     lib.lora_paged_attn_fwd.argtypes = [P, CA, P, P, P, I64, I32] + [I64] * 7 + [F, I32, P, P, SZ, P]
     lib.lora_paged_attn_workspace_bytes.argtypes = [CA, I64, I32, I64, I64, I64, I32]
     for f in ("lora_qk_norm_rope_workspace_bytes", "lora_paged_attn_workspace_bytes"):
         getattr(lib, f).restype = SZ
     for f in ("lora_requests_fwd", "lora_qk_norm_rope_fwd", "lora_qk_norm_rope_bwd", "lora_kv_cache_write", "lora_kv_cache_read",
-              "lora_paged_attn_fwd"):
+              "lora_paged_attn_fwd", "lora_weights_write", "lora_weights_read", "lora_requests_quantised_fwd", "lora_kv_cache_append"):
         getattr(lib, f).restype = C.c_int
     for f in ("lora_fwd", "lora_bwd", "multi_lora_fwd", "multi_lora_bwd", "multi_lora_fwd_ranked",
               "multi_lora_bwd_ranked", "lora_debug_mask",
@@ -369,7 +374,8 @@ def ceiling_hbm_read(src, sink, workgroups) -> int:
 
 # ---- serving adapters, and what stands behind the query and key projections -----------------------------
 # (a decode step's launches run for 3 - 5 us each: the checks look at every tensor once, and pointers go as numbers)
-_BF16, _F32, _I32, _FP8 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+_BF16, _F32, _I32, _FP8, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn, torch.uint8
+KV_FP4 = -4                            # LORA_KV_FP4 in the header
 
 
 def _at(t: torch.Tensor, dtype) -> int:
@@ -399,6 +405,46 @@ def lora_requests_fwd(X, W, A, B, ids, s, ranks=None, Y=None, S=None):
     _check(load_library().lora_requests_fwd(_at(X, _BF16), _at(W, _BF16), _at(A, _BF16), _at(B, _BF16), _at(ids, _I32),
                                             None if ranks is None else _at(ranks, _I32), _at(s, _F32), M, K, N, r, P, _at(Y, _BF16),
                                             _at(S, _BF16), _stream()))
+    return Y, S
+
+
+def lora_weights_write(W, codes=None, exps=None):
+    """codes [N,K/2], exps [N,K/32] (uint8): W [N,K] bf16 in 4 bits with a power of two for every 32 entries of a row."""
+    N, K = W.shape
+    codes = torch.empty((N, K // 2), dtype=_U8, device=W.device) if codes is None else codes
+    exps = torch.empty((N, K // 32), dtype=_U8, device=W.device) if exps is None else exps
+    assert codes.shape == (N, K // 2) and exps.shape == (N, K // 32), "shapes do not fit"
+    _check(load_library().lora_weights_write(_at(W, _BF16), N, K, _at(codes, _U8), _at(exps, _U8), _stream()))
+    return codes, exps
+
+
+def lora_weights_read(codes, exps, W=None):
+    """W [N,K] bf16, exactly what codes and exps hold: for lora_fwd, lora_bwd and the like over the same frozen weights."""
+    N, K = codes.shape[0], 2 * codes.shape[1]
+    W = torch.empty((N, K), dtype=_BF16, device=codes.device) if W is None else W
+    assert W.shape == (N, K) and exps.shape == (N, K // 32), "shapes do not fit"
+    _check(load_library().lora_weights_read(_at(codes, _U8), _at(exps, _U8), N, K, _at(W, _BF16), _stream()))
+    return W
+
+
+def lora_requests_quantised_fwd(X, codes, exps, A=None, B=None, ids=None, s=None, ranks=None, Y=None, S=None):
+    """lora_requests_fwd over weights in 4 bits (codes, exps: lora_weights_write).  Without A, B, ids and s: no adapters, and S is None."""
+    M, K = X.shape
+    N = codes.shape[0]
+    Y = torch.empty((M, N), dtype=_BF16, device=X.device) if Y is None else Y
+    assert codes.shape == (N, K // 2) and exps.shape == (N, K // 32) and Y.shape == (M, N), "shapes do not fit"
+    if A is None:
+        assert B is None and ids is None and s is None and ranks is None, "adapters are A, B, ids and s together"
+        _check(load_library().lora_requests_quantised_fwd(_at(X, _BF16), _at(codes, _U8), _at(exps, _U8), None, None, None, None, None, M, K, N, 0, 0,
+                                                          _at(Y, _BF16), None, _stream()))
+        return Y, None
+    P, _, r = B.shape
+    S = torch.empty((M, r), dtype=_BF16, device=X.device) if S is None else S
+    assert A.shape == (P, r, K) and B.shape == (P, N, r) and ids.numel() == M and s.numel() == P and (ranks is None or ranks.numel() == P) and \
+        S.shape == (M, r), "shapes do not fit"
+    _check(load_library().lora_requests_quantised_fwd(_at(X, _BF16), _at(codes, _U8), _at(exps, _U8), _at(A, _BF16), _at(B, _BF16), _at(ids, _I32),
+                                                      None if ranks is None else _at(ranks, _I32), _at(s, _F32), M, K, N, r, P, _at(Y, _BF16),
+                                                      _at(S, _BF16), _stream()))
     return Y, S
 
 
@@ -449,27 +495,33 @@ def lora_qk_norm_rope_bwd(q, k, gq, gk, cos, sin, pos, dq_out, dk_out, eps=1e-6,
 
 class KVCache:
     """A paged cache over tensors that the caller holds: k, v [pages, heads, page, dim], bf16, or fp8 (torch.float8_e4m3fn) with
-    the biased exponents k_exp, v_exp [pages, heads, page] (uint8) of a power of two for every token and head."""
+    the biased exponents k_exp, v_exp [pages, heads, page] (uint8) of a power of two for every token and head, or 4 bits: k, v [pages, heads, page, dim/2]
+    (uint8, two codes to a byte) with k_exp, v_exp [pages, heads, page, dim/32] of a power of two for every 32 entries."""
     __slots__ = ("tensors", "pages", "heads", "page", "dim", "_c", "_ref")
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
         shape = k.shape
         assert len(shape) == 4 and v.shape == shape, "k and v are [pages, heads, page, dim]"
         self.pages, self.heads, self.page, self.dim = shape
-        if k.dtype is _FP8:
-            assert k_exp is not None and v_exp is not None and k_exp.shape == v_exp.shape == shape[:3], "an exponent for every token and head"
+        form, exps = {_FP8: (1, shape[:3]), _U8: (KV_FP4, (*shape[:3], shape[3] // 16))}.get(k.dtype, (0, None))
+        if form == KV_FP4:
+            self.dim *= 2
+        if form:
+            assert k_exp is not None and v_exp is not None and k_exp.shape == v_exp.shape == exps, "exponents: one for every token and head, 4 bits for every 32 entries"
             self.tensors = (k, v, k_exp, v_exp)
-            self._c = CacheArrays(_at(k, _FP8), _at(v, _FP8), _at(k_exp, torch.uint8), _at(v_exp, torch.uint8), shape[0], shape[2], shape[1], shape[3],
-                                  1)
+            self._c = CacheArrays(_at(k, k.dtype), _at(v, k.dtype), _at(k_exp, _U8), _at(v_exp, _U8), shape[0], shape[2], shape[1], self.dim, form)
         else:
             self.tensors = (k, v, None, None)
             self._c = CacheArrays(_at(k, _BF16), _at(v, _BF16), None, None, shape[0], shape[2], shape[1], shape[3], 0)
         self._ref = C.byref(self._c)
 
     @classmethod
-    def empty(cls, pages, page, heads, dim, fp8=False, device="cuda"):
-        k, v = (torch.zeros((pages, heads, page, dim), dtype=_FP8 if fp8 else _BF16, device=device) for _ in range(2))
-        exps = (torch.zeros((pages, heads, page), dtype=torch.uint8, device=device) for _ in range(2)) if fp8 else (None, None)
+    def empty(cls, pages, page, heads, dim, fp8=False, device="cuda", fp4=False):
+        assert not (fp8 and fp4), "fp8 or fp4"
+        width, dtype = (dim // 2, _U8) if fp4 else (dim, _FP8 if fp8 else _BF16)
+        k, v = (torch.zeros((pages, heads, page, width), dtype=dtype, device=device) for _ in range(2))
+        shape = (pages, heads, page, dim // 32) if fp4 else (pages, heads, page)
+        exps = (torch.zeros(shape, dtype=_U8, device=device) for _ in range(2)) if fp8 or fp4 else (None, None)
         return cls(k, v, *exps)
 
 
@@ -493,6 +545,24 @@ def lora_kv_cache_read(cache: KVCache, slots, k=None, v=None):
     vp, ldv = _heads(v)
     _check(load_library().lora_kv_cache_read(cache._ref, _at(slots, torch.int64), M, kp, vp, ldk, ldv, _stream()))
     return k, v
+
+
+def lora_kv_cache_append(cache: KVCache, q, k, v, cos, sin, pos, slots, gq=None, gk=None, eps=1e-6, interleaved=False, q_out=None):
+    """q_out [M,H,D]: lora_qk_norm_rope_fwd and lora_kv_cache_write in one call: queries out, keys and v [M, heads, dim] (rows may be apart) to their slots; without gq
+    and gk no norm, the rotation alone."""
+    M, H, D = q.shape
+    positions, half = cos.shape
+    q_out = torch.empty((M, H, D), dtype=_BF16, device=q.device) if q_out is None else q_out
+    assert D == cache.dim and k.shape == v.shape == (M, cache.heads, D) and cos.shape == sin.shape and pos.numel() == M and slots.numel() == M and \
+        q_out.shape == q.shape and (gq is None or gq.numel() == D) and (gk is None or gk.numel() == D), "shapes do not fit"
+    qp, ldq = _heads(q)
+    kp, ldk = _heads(k)
+    vp, ldv = _heads(v)
+    qo, ldqo = _heads(q_out)
+    _check(load_library().lora_kv_cache_append(cache._ref, qp, kp, vp, None if gq is None else _at(gq, _BF16), None if gk is None else _at(gk, _BF16),
+                                               _at(cos, _F32), _at(sin, _F32), _at(pos, _I32), _at(slots, torch.int64), M, H, 2 * half, positions, ldq,
+                                               ldk, ldv, ldqo, eps, interleaved, qo, _stream()))
+    return q_out
 
 
 def alloc_paged_attn_workspace(cache: KVCache, T, H, seqs, max_new, max_kv, window=0, device="cuda") -> torch.Tensor:

@@ -15,7 +15,7 @@
 // keys in LDS, 32 rows to a wave.  Long key ranges of few tiles are cut into parts for more workgroups, whose results
 // attn_join_kernel adds.
 //
-// The fp8 form of the cache is widened to bf16 (exact: e4m3 times a power of two) on the way to LDS or into the fragments.
+// The fp8 and 4-bit forms of the cache are widened to bf16 (exact: e4m3 or e2m1 times a power of two) on the way to LDS or into the fragments.
 #include <algorithm>
 #include <type_traits>
 
@@ -87,6 +87,14 @@ __device__ __forceinline__ int64_t attn_block(const AttnArgs& p, const AttnTile&
 __device__ __forceinline__ int block_key(const AttnTile& t, int key, int b) { return min(key + 16 * b, t.k1 - 1) & ~15; }
 
 __device__ __forceinline__ float scale_of(uint8_t e) { return ldexpf(1.f, (int)e - 127); }
+
+// A head of one token as the cache holds it: bytes of its entries, 16-byte chunks of them, exponents.
+template <int D, int FORM>
+struct Held {
+    static constexpr int BYTES = FORM == kCacheBf16 ? 2 * D : FORM == kCacheFp8 ? D : D / 2, CHUNKS = BYTES / 16;
+    static constexpr int EXPS = FORM == kCacheFp4 ? D / 32 : 1;
+    static constexpr int WIDE = FORM == kCacheBf16 ? 1 : FORM == kCacheFp8 ? 2 : 4;        // chunks of bf16 that a chunk is widened to
+};
 
 // Eight e4m3 values times a power of two.
 __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
@@ -253,18 +261,21 @@ __device__ __forceinline__ u32x4 not_finite(u32x4 v) {       // 0xFFFF in the ha
     }
     return m;
 }
-template <int D, bool FP8, int NQ, int KB>
+template <int D, int FORM, int NQ, int KB>
 __device__ __forceinline__ void add_not_finite(const AttnArgs& p, const AttnTile& t, f32x4 (&o)[NQ][D / 16], const int (&pos)[NQ], int key0) {
     const int q = lane_here() >> 4;
 #pragma unroll 1
     for (int k = 0; k < min(16 * KB, t.k1 - key0); ++k) {
         const int at16 = (key0 + k) & ~15;
         const int64_t at = attn_block(p, t, page_of(p, t, at16), at16) + (k & 15);
-        const char* row = (const char*)p.c.v + at * (D * (FP8 ? 1 : 2)) + q * (FP8 ? 4 : 8);
+        constexpr int FOUR = Held<D, FORM>::BYTES * 4 / D;                        // bytes of four entries
+        const char* row = (const char*)p.c.v + at * Held<D, FORM>::BYTES + q * FOUR;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
             u32x2 x;
-            if constexpr (FP8) {
+            if constexpr (FORM == kCacheFp4) {
+                x = __builtin_bit_cast(u32x4, from_fp4(*(const uint16_t*)(row + 8 * d), exp2_of_biased(p.c.v_exp[at * (D / 32) + d / 2]))).xy;
+            } else if constexpr (FORM == kCacheFp8) {
                 const uint32_t y = *(const uint32_t*)(row + 16 * d);
                 x = __builtin_bit_cast(u32x4, widen8(y, y, scale_of(p.c.v_exp[at]))).xy;
             } else {
@@ -324,19 +335,21 @@ __device__ __forceinline__ void have(bf16x8 (&f)[N]) {
 // one.  Measured (a read of 2 GiB: 6.0 TB/s): four sequences of 33000 - 131072 keys, bf16, 1.34 GB, 229 us, 5.9 TB/s; 32 of 200 - 4000, fp8, 139 MB, 32 us, 4.3 TB/s,
 // some 6 us of it until the first keys are there (lengths, page numbers, keys: one after the other).  Two tiles of fp8 under way, with the registers that
 // takes, 41 us for the latter launch and the join instead of 37.
-template <int D, bool FP8, int NQ>
+template <int D, int FORM, int NQ>
 struct Few {
     static constexpr int KEYS = 32, WAVES = 4;
-    static constexpr int KL = 2 * D / (FP8 ? 64 : 32);             // 16-byte loads of a lane for the keys of a tile
-    static constexpr int VL = KEYS * D * (FP8 ? 1 : 2) / 1024;     // ... for the values
+    static constexpr int KL = FORM == kCacheFp4 ? 2 : Held<D, FORM>::CHUNKS / 2;   // loads of a lane for the keys of a tile, 16 bytes (4 bits of 64 entries: 8)
+    static constexpr int VL = KEYS * Held<D, FORM>::BYTES / 1024;                  // ... for the values
     static constexpr int V_BYTES = KEYS * D * 2, O_BYTES = 16 * NQ * D * 4;
     static constexpr int WAVE_LDS = V_BYTES > O_BYTES ? V_BYTES : O_BYTES;
     static constexpr int BASE = WAVES * WAVE_LDS + WAVES * NQ * 16 * 8, LDS = BASE + WAVES * NQ * 16 * 4;
 };
 
-template <int D, bool FP8, int NQ>
+template <int D, int FORM, int NQ>
 __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs p) {
-    using C = Few<D, FP8, NQ>;
+    using C = Few<D, FORM, NQ>;
+    using H = Held<D, FORM>;
+    constexpr bool FP8 = FORM == kCacheFp8, FP4 = FORM == kCacheFp4;
     constexpr int KK = D / 32, DB = D / 16;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     AttnTile t;
@@ -346,7 +359,8 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
     float* base = (float*)(smem + C::BASE) + w * NQ * 16;
     int far = 0;
 
-    // queries: step kk holds entries 32 kk + 8 q .. + 7, fp8 64 (kk / 2) + 16 q + 8 (kk & 1) .. + 7 (as a 16-byte load of a key brings them)
+    // queries: step kk holds entries 32 kk + 8 q .. + 7, fp8 64 (kk / 2) + 16 q + 8 (kk & 1) .. + 7, 4 bits (D / 4) q + 8 kk .. + 7 (as a load of a key
+    // brings them)
     bf16x8 qf[NQ][KK];
     int pos[NQ];
 #pragma unroll
@@ -356,7 +370,7 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
         const lora_bf16* src = q_row(p, t, row);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk)
-            qf[i][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(src + (FP8 ? 64 * (kk / 2) + 16 * q + 8 * (kk & 1) : 32 * kk + 8 * q)));
+            qf[i][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(src + (FP4 ? D / 4 * q + 8 * kk : FP8 ? 64 * (kk / 2) + 16 * q + 8 * (kk & 1) : 32 * kk + 8 * q)));
     }
     const int pos_lo = pos_of(p, t, t.row0);
 #pragma unroll
@@ -374,7 +388,7 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
     u32x4 kr[C::KL], vr[C::VL];
     uint8_t ke[2], ve[C::VL];
     const char *kc = (const char*)p.c.k, *vc = (const char*)p.c.v;
-    constexpr int ESZ = FP8 ? 1 : 2, LANES = D * ESZ / 16;          // lanes to a row of values
+    constexpr int LANES = H::CHUNKS;                        // lanes to a row of values
     int pages[2];                                           // of the blocks of the tile that is asked for next
     int64_t blk[2];
     auto look_up = [&](int key) {
@@ -389,9 +403,14 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int64_t at = blk[b] + c;
+            if constexpr (FP4 && D == 64) {
+                kr[b].xy = *(const u32x2*)(kc + at * H::BYTES + 8 * q);
+            } else {
 #pragma unroll
-            for (int i = 0; i < C::KL / 2; ++i) kr[b * (C::KL / 2) + i] = *(const u32x4*)(kc + at * (D * ESZ) + 64 * i + 16 * q);
+                for (int i = 0; i < C::KL / 2; ++i) kr[b * (C::KL / 2) + i] = *(const u32x4*)(kc + at * H::BYTES + 64 * i + 16 * q);
+            }
             if constexpr (FP8) ke[b] = p.c.k_exp[at];
+            if constexpr (FP4) ke[b] = p.c.k_exp[at * H::EXPS + q * H::EXPS / 4];
         }
     };
     auto load_v = [&]() {
@@ -399,8 +418,9 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
         for (int i = 0; i < C::VL; ++i) {
             const int row = i * (64 / LANES) + l / LANES;
             const int64_t at = (row < 16 ? blk[0] : blk[1]) + (row & 15);
-            vr[i] = *(const u32x4*)(vc + at * (D * ESZ) + l % LANES * 16);
+            vr[i] = *(const u32x4*)(vc + at * H::BYTES + l % LANES * 16);
             if constexpr (FP8) ve[i] = p.c.v_exp[at];
+            if constexpr (FP4) ve[i] = p.c.v_exp[at * H::EXPS + l % LANES];
         }
     };
 
@@ -423,30 +443,29 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
         for (int i = 0; i < C::VL; ++i) {
             const int row = i * (64 / LANES) + l / LANES, ch = l % LANES;
             const bool in = key + row < t.k1;
-            u32x4 lo = vr[i], hi;
-            if constexpr (FP8) {
+            u32x4 wide[H::WIDE];
+            if constexpr (FP4) {
+                const float sc = exp2_of_biased(ve[i]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) wide[e] = __builtin_bit_cast(u32x4, from_fp4(vr[i][e], sc));
+            } else if constexpr (FP8) {
                 const float sc = scale_of(ve[i]);
-                lo = __builtin_bit_cast(u32x4, widen8(vr[i][0], vr[i][1], sc));
-                hi = __builtin_bit_cast(u32x4, widen8(vr[i][2], vr[i][3], sc));
+                wide[0] = __builtin_bit_cast(u32x4, widen8(vr[i][0], vr[i][1], sc));
+                wide[1] = __builtin_bit_cast(u32x4, widen8(vr[i][2], vr[i][3], sc));
+            } else {
+                wide[0] = vr[i];
             }
             if (!whole) {
-                lo = in ? lo : u32x4{0u, 0u, 0u, 0u};
-                u32x4 m = not_finite(lo);
-                lo &= ~m;
-                if constexpr (FP8) {
-                    hi = in ? hi : u32x4{0u, 0u, 0u, 0u};
-                    const u32x4 mh = not_finite(hi);
-                    hi &= ~mh;
-                    m |= mh;
+#pragma unroll
+                for (int e = 0; e < H::WIDE; ++e) {
+                    wide[e] = in ? wide[e] : u32x4{0u, 0u, 0u, 0u};
+                    const u32x4 m = not_finite(wide[e]);
+                    wide[e] &= ~m;
+                    bad |= (m[0] | m[1] | m[2] | m[3]) != 0;
                 }
-                bad |= (m[0] | m[1] | m[2] | m[3]) != 0;
             }
-            if constexpr (FP8) {
-                *(u32x4*)(mine + v_off<D>(row, 2 * ch)) = lo;
-                *(u32x4*)(mine + v_off<D>(row, 2 * ch + 1)) = hi;
-            } else {
-                *(u32x4*)(mine + v_off<D>(row, ch)) = lo;
-            }
+#pragma unroll
+            for (int e = 0; e < H::WIDE; ++e) *(u32x4*)(mine + v_off<D>(row, H::WIDE * ch + e)) = wide[e];
         }
         if (more) {
             find(key + STEP);
@@ -461,7 +480,9 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
                 bf16x8 kf;
-                if constexpr (FP8) {
+                if constexpr (FP4) {
+                    kf = from_fp4(kr[b][kk], exp2_of_biased(ke[b]));
+                } else if constexpr (FP8) {
                     const u32x4 r = kr[b * (C::KL / 2) + kk / 2];
                     kf = kk & 1 ? widen8(r[2], r[3], scale_of(ke[b])) : widen8(r[0], r[1], scale_of(ke[b]));
                 } else {
@@ -501,7 +522,7 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
         }
         asm volatile("" ::: "memory");
         add_values<D, NQ>(o, pf, mine);
-        if (__any(bad)) add_not_finite<D, FP8, NQ, 2>(p, t, o, pos, key);
+        if (__any(bad)) add_not_finite<D, FORM, NQ, 2>(p, t, o, pos, key);
     }
 
     // the four waves' sums, brought to one reference
@@ -560,12 +581,13 @@ constexpr int slots_before(int n, int items, int slots) { return n <= 0 ? 0 : n 
 // ones, two to each: only those of the same wave run beside a matrix instruction, those of other waves wait for it.  Measured: two
 // prompts' 1021 new tokens over 5003 and 16000 keys, 32 heads of 128 to 8, 250 GFLOP, 265 us, 940 TFLOP/s (a product of 8192^3: 1320); bound by the issue of
 // instructions (a step of 64 keys takes 3300 cycles, of which its 64 matrix instructions and the 64 of the SIMD's other wave 2050).
-template <int D, bool FP8>
+template <int D, int FORM>
 struct Many {
     static constexpr int KEYS = 64, ROWS = 128, NQ = 2;
-    // two tiles of keys, two of values; flags; of every row the score that it counts from; fp8 a tile as it is held
+    // two tiles of keys, two of values; flags; of every row the score that it counts from; fp8, 4 bits: a tile as it is held
+    static constexpr int WAVE_RAW = FORM == kCacheBf16 ? 0 : 16 * Held<D, FORM>::BYTES < 1024 ? 1024 : 16 * Held<D, FORM>::BYTES;   // (a copy brings 1 KB)
     static constexpr int TILE = KEYS * D * 2, FLAGS = 4 * TILE, BASE = FLAGS + 16, RAW = BASE + ROWS * 4;
-    static constexpr int LDS = RAW + (FP8 ? KEYS * D : 0);
+    static constexpr int LDS = RAW + 4 * WAVE_RAW;
 };
 
 // Copy I of a block of 16 keys (or values) into LDS, 1 KB: the instruction's offset, the same for memory and LDS, counts from the middle.  The first
@@ -592,9 +614,11 @@ __device__ __forceinline__ void copy_raw(const char* from, uint32_t lane, uint32
     }
 }
 
-template <int D, bool FP8>
+template <int D, int FORM>
 __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
-    using C = Many<D, FP8>;
+    using C = Many<D, FORM>;
+    using H = Held<D, FORM>;
+    constexpr bool RAW = FORM != kCacheBf16;
     constexpr int NQ = C::NQ, KK = D / 32, DB = D / 16, KB = C::KEYS / 16;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     AttnTile t;
@@ -625,7 +649,7 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
     }
 
     // Straight into LDS, wave w the 16 keys of block w, which lie side by side in their page; a lane's source chosen so that what it writes lies
-    // swizzled.  fp8: as it is, into a place of the wave's own, from where the wave widens it into the tile.
+    // swizzled.  fp8, 4 bits: as it is, into a place of the wave's own, from where the wave widens it into the tile.
     constexpr int RPC = 512 / D;                             // bf16: rows of a 1 KB copy
     const uint32_t lds = lds_addr_of(smem);
     // source of a lane in copy 0; in copy i, 1 KB further, only the swizzle differs, by a constant: k_off, v_off of row RPC * i
@@ -633,45 +657,56 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
         const int le = lane_here(), row = le / (D / 8);
         return (uint32_t)((row * 2 * D + le % (D / 8) * 16) ^ ((keys ? k_off<D>(row, 0) : v_off<D>(row, 0)) & (2 * D - 1)));
     };
-    constexpr int NR = FP8 ? D / 64 : 1, RPR = 1024 / D;     // fp8: copies of a block, rows of one
-    uint8_t ex[NR];                                         // ... and of this lane's row of each the exponent
+    constexpr int RPR = 1024 / H::BYTES < 16 ? 1024 / H::BYTES : 16, NR = 16 / RPR;     // fp8, 4 bits: rows of a copy, copies of a block
+    constexpr int RAW_LANES = RPR * H::CHUNKS;              // ... lanes that have something of it (the others bring the same again)
+    uint8_t ex[NR];                                         // ... and of this lane's chunk of each the exponent
     // first head entry of the wave's block in the tiles whose values (at_v) and keys (at_k) are asked for next, and in the one between; page of the
     // one after
     int64_t at_v, at_n, at_k;
     int page_after;
     auto page_at = [&](int key) { return page_of(p, t, block_key(t, key, w)); };
     auto block_at = [&](int page, int key) { return attn_block(p, t, page, block_key(t, key, w)); };
-    auto source = [&](bool keys, int64_t at) { return (const char*)(keys ? p.c.k : p.c.v) + at * (FP8 ? D : 2 * D); };
+    auto source = [&](bool keys, int64_t at) { return (const char*)(keys ? p.c.k : p.c.v) + at * H::BYTES; };
     // keys (values) into half `stage` of their part of LDS
     auto bring = [&](bool keys, int64_t at, int stage) {
         const char* from = source(keys, at);
-        if constexpr (FP8) {
-            copy_raw<NR>(from, lane_here() * 16, __builtin_amdgcn_readfirstlane(lds + C::RAW + w * 16 * D));
+        if constexpr (RAW) {
+            const int le = lane_here() % RAW_LANES;
+            copy_raw<NR>(from, le * 16, __builtin_amdgcn_readfirstlane(lds + C::RAW + w * C::WAVE_RAW));
 #pragma unroll
-            for (int i = 0; i < NR; ++i) ex[i] = (keys ? p.c.k_exp : p.c.v_exp)[at + i * RPR + lane_here() / (D / 16)];
+            for (int i = 0; i < NR; ++i)
+                ex[i] = (keys ? p.c.k_exp : p.c.v_exp)[(at + i * RPR + le / H::CHUNKS) * H::EXPS + le % H::CHUNKS * H::EXPS / H::CHUNKS];
         } else {
             const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds + (keys ? 0 : 2 * C::TILE) + stage * C::TILE + w * 32 * D + D / 64 * 1024);
             if (keys) copy_block<D, true>(from, lane_source(true), m0);
             else copy_block<D, false>(from, lane_source(false), m0);
         }
     };
-    // fp8: row and first chunk in the tile of 16 bytes of copy i, and what they are widened to
-    struct Wide { int row, chunk; u32x4 lo, hi; };
+    // fp8, 4 bits: row and first chunk in the tile of 16 bytes of copy i, and what they are widened to
+    struct Wide { int row, chunk; u32x4 v[H::WIDE]; };
     auto widened = [&](int i) {
-        const int le = lane_here();
-        const u32x4 raw = *(const u32x4*)(smem + C::RAW + w * 16 * D + i * 1024 + le * 16);
-        const float sc = scale_of(ex[i]);
-        return Wide{16 * w + i * RPR + le / (D / 16), le % (D / 16) * 2, __builtin_bit_cast(u32x4, widen8(raw[0], raw[1], sc)),
-                    __builtin_bit_cast(u32x4, widen8(raw[2], raw[3], sc))};
+        const int le = lane_here() % RAW_LANES;
+        const u32x4 raw = *(const u32x4*)(smem + C::RAW + w * C::WAVE_RAW + i * 1024 + le * 16);
+        Wide x{16 * w + i * RPR + le / H::CHUNKS, le % H::CHUNKS * H::WIDE, {}};
+        if constexpr (FORM == kCacheFp4) {
+            const float sc = exp2_of_biased(ex[i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x.v[e] = __builtin_bit_cast(u32x4, from_fp4(raw[e], sc));
+        } else if constexpr (FORM == kCacheFp8) {
+            const float sc = scale_of(ex[i]);
+            x.v[0] = __builtin_bit_cast(u32x4, widen8(raw[0], raw[1], sc));
+            x.v[1] = __builtin_bit_cast(u32x4, widen8(raw[2], raw[3], sc));
+        }
+        return x;
     };
     auto brought_k = [&](int stage) {
         wait_slab_loads();
-        if constexpr (FP8)
+        if constexpr (RAW)
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 const Wide x = widened(i);
-                *(u32x4*)(smem + stage * C::TILE + k_off<D>(x.row, x.chunk)) = x.lo;
-                *(u32x4*)(smem + stage * C::TILE + k_off<D>(x.row, x.chunk + 1)) = x.hi;
+#pragma unroll
+                for (int e = 0; e < H::WIDE; ++e) *(u32x4*)(smem + stage * C::TILE + k_off<D>(x.row, x.chunk + e)) = x.v[e];
             }
     };
     // flag of a stage: the number of its tile if a value in it is not finite, where that matters (a tile that not all rows see in whole)
@@ -692,16 +727,15 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
             return x & ~m;
         };
         wait_slab_loads();
-        if constexpr (FP8) {
+        if constexpr (RAW) {
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 Wide x = widened(i);
-                if (guard) {
-                    x.lo = guarded(x.lo, x.row);
-                    x.hi = guarded(x.hi, x.row);
+#pragma unroll
+                for (int e = 0; e < H::WIDE; ++e) {
+                    if (guard) x.v[e] = guarded(x.v[e], x.row);
+                    *(u32x4*)(st + v_off<D>(x.row, x.chunk + e)) = x.v[e];
                 }
-                *(u32x4*)(st + v_off<D>(x.row, x.chunk)) = x.lo;
-                *(u32x4*)(st + v_off<D>(x.row, x.chunk + 1)) = x.hi;
             }
         } else if (guard) {
             for (int i = lane_here(); i < 2 * D; i += 64) {  // the wave's own 16 rows, chunk by chunk
@@ -795,7 +829,7 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
         const char *from_k = nullptr, *from_v = nullptr;
         uint32_t lane_k = 0, lane_v = 0, m0_k = 0, m0_v = 0;
         const int64_t at_v_now = at_v;
-        if constexpr (FP8) {
+        if constexpr (RAW) {
             bring(true, at_k, stage);
         } else {
             from_k = source(true, at_k);
@@ -846,19 +880,19 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
                 at_k = block_at(page_after, key + 3 * C::KEYS);
                 page_after = page_at(key + 4 * C::KEYS);
             }
-            if constexpr (!FP8 && n % EVERY == EVERY - 1 && n / EVERY < 2 * NP) {
+            if constexpr (!RAW && n % EVERY == EVERY - 1 && n / EVERY < 2 * NP) {
                 constexpr int j = n / EVERY;
                 if constexpr (j < NP) copy_one<D, true, j>(from_k, lane_k, m0_k);
                 else copy_one<D, false, j - NP>(from_v, lane_v, m0_v);
             }
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (FP8 && n == NS - 1) {             // (one place for what is to be widened)
+            if constexpr (RAW && n == NS - 1) {             // (one place for what is to be widened)
                 brought_k(stage);
                 bring(false, at_v_now, stage);
             }
         });
         if (key > t.k0 && !all_whole(key - C::KEYS) && flags[stage ^ 1] == key - C::KEYS)
-            add_not_finite<D, FP8, NQ, KB>(p, t, o, pos, key - C::KEYS);
+            add_not_finite<D, FORM, NQ, KB>(p, t, o, pos, key - C::KEYS);
         if (moved) {
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
@@ -884,7 +918,7 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
         for (int f = 0; f < AHEAD; ++f) read_v(f);
 #pragma unroll
         for (int n = 0; n < NV; ++n) value(wb, n);
-        if (flags[1] == key - C::KEYS) add_not_finite<D, FP8, NQ, KB>(p, t, o, pos, key - C::KEYS);
+        if (flags[1] == key - C::KEYS) add_not_finite<D, FORM, NQ, KB>(p, t, o, pos, key - C::KEYS);
     }
     if (far) count_from_zero(m, base, lane_here() & 15, p.scale);
 #pragma unroll
@@ -1038,11 +1072,16 @@ static hipError_t launch_lds(int lds, unsigned blocks, const AttnArgs& a, hipStr
     return hipGetLastError();
 }
 
-template <int D, bool FP8>
+template <int D, int FORM>
 static hipError_t launch_attn_t(const AttnArgs& a, int rows, unsigned blocks, hipStream_t st) {
-    if (rows == 16) return launch_lds<attn_few_kernel<D, FP8, 1>>(Few<D, FP8, 1>::LDS, blocks, a, st);
-    if (rows == 32) return launch_lds<attn_few_kernel<D, FP8, 2>>(Few<D, FP8, 2>::LDS, blocks, a, st);
-    return launch_lds<attn_many_kernel<D, FP8>>(Many<D, FP8>::LDS, blocks, a, st);
+    if (rows == 16) return launch_lds<attn_few_kernel<D, FORM, 1>>(Few<D, FORM, 1>::LDS, blocks, a, st);
+    if (rows == 32) return launch_lds<attn_few_kernel<D, FORM, 2>>(Few<D, FORM, 2>::LDS, blocks, a, st);
+    return launch_lds<attn_many_kernel<D, FORM>>(Many<D, FORM>::LDS, blocks, a, st);
+}
+template <int D>
+static hipError_t launch_attn_d(const AttnArgs& a, int rows, unsigned blocks, hipStream_t st) {
+    if (a.c.form == kCacheFp4) return launch_attn_t<D, kCacheFp4>(a, rows, blocks, st);
+    return a.c.form == kCacheFp8 ? launch_attn_t<D, kCacheFp8>(a, rows, blocks, st) : launch_attn_t<D, kCacheBf16>(a, rows, blocks, st);
 }
 
 template <int D>
@@ -1060,9 +1099,7 @@ hipError_t launch_attn(AttnArgs a, const AttnPlan& p, int max_new, hipStream_t s
     a.splits = p.splits;
     a.split_keys = p.split_keys;
     const unsigned blocks = (unsigned)((int64_t)a.tiles * a.splits * a.B * a.c.heads);
-    hipError_t e;
-    if (a.c.D == 64) e = a.c.fp8 ? launch_attn_t<64, true>(a, p.rows, blocks, st) : launch_attn_t<64, false>(a, p.rows, blocks, st);
-    else e = a.c.fp8 ? launch_attn_t<128, true>(a, p.rows, blocks, st) : launch_attn_t<128, false>(a, p.rows, blocks, st);
+    const hipError_t e = a.c.D == 64 ? launch_attn_d<64>(a, p.rows, blocks, st) : launch_attn_d<128>(a, p.rows, blocks, st);
     if (e != hipSuccess || a.splits == 1) return e;
     return a.c.D == 64 ? launch_join<64>(a, p.rows, max_new, st) : launch_join<128>(a, p.rows, max_new, st);
 }

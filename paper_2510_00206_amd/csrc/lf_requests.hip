@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestTi
 // tiles, with four columns to a wave: 3 rows, K = 1024 2.7 / 3.4; 64 rows of 48 adapters, K = 4096, r = 16 4.0 / 6.2; 200 rows of 106 adapters, r = 64 13.8 / 16.5.
 // (Whole layer, 4096 -> 4096, one adapter: 128 rows, r = 16 15.5 / 21.6; 512 rows 28.0 / 31.7; r = 64, 256 rows 25.4 / 26.2, 512 rows 38.4 / 33.5; an adapter for
 // each row: level.)  With two: 2.7, 3.9, 12.4 (27 MB, 2.2 TB/s); 2048 rows on tiles 12.4 (17 MB of X).
-static hipError_t launch_request_down(const RequestDownArgs& a, hipStream_t st) {
+static hipError_t launch_down(const RequestDownArgs& a, hipStream_t st) {
     if (a.M <= 512 && a.M * a.r <= 512 * 32) {
         hipLaunchKernelGGL(request_rows_kernel, dim3((unsigned)a.M, (unsigned)a.r / kDownColumns), dim3(64), 0, st, a);
         return hipGetLastError();
@@ -151,8 +151,12 @@ static hipError_t launch_request_down(const RequestDownArgs& a, hipStream_t st) 
     return hipSuccess;
 }
 
+hipError_t launch_request_down(const RequestArgs& a, hipStream_t st) {
+    return launch_down(RequestDownArgs{a.X, a.A, a.ids, a.ranks, a.s, a.S, a.M, a.K, a.r, a.P}, st);
+}
+
 hipError_t launch_requests(const RequestArgs& a, hipStream_t st) {
-    hipError_t e = launch_request_down(RequestDownArgs{a.X, a.A, a.ids, a.ranks, a.s, a.S, a.M, a.K, a.r, a.P}, st);
+    hipError_t e = launch_request_down(a, st);
     RingPart part[2];
     const int n = plan_ring(a.M, a.K, a.N, part);
     for (int i = 0; i < n && e == hipSuccess; ++i) {

@@ -12,7 +12,7 @@
 // 4.7 of them the sum of its planes; forward of 16 rows 4 us: the launch, and position, table and row read one after the other.
 #include <algorithm>
 
-#include "lf_serve.h"
+#include "lf_rope_parts.h"
 
 namespace lf {
 
@@ -21,82 +21,6 @@ constexpr int kRopeThreads = 256;
 // (32 lanes to a head) three.  us, of 4 / 8 / 16 waves: 5003 rows of 64 + 8 heads 60.9 / 63.6 / 65.5, 16000 rows of 32 + 8 100 / 105 / 105.
 constexpr int kRopeBlocks = 4 * kComputeUnits;
 constexpr int rope_bwd_waves(int lanes) { return lanes == 32 ? 3 : 4; }
-
-// GL lanes to a head, a wave for a row, or for a part of its heads.
-template <int GL, bool INTER>
-struct RopeLane {
-    int j, slot;                       // lane of the head, head of the wave
-    bool active, turned;               // ... has entries; they are in the rotated part
-    int at, other;                     // first index into a row of the tables; wave lane with the other entries of this one's pairs
-    float sign;                        // of the sine in y: - for the first entry of a pair
-    __device__ __forceinline__ RopeLane(int D, int rot) {
-        const int l = threadIdx.x & 63;
-        j = l % GL;
-        slot = l / GL;
-        active = 8 * j < D;
-        turned = 8 * j < rot;
-        const bool first = INTER || 8 * j < rot / 2;
-        at = INTER ? 4 * j : first ? 8 * j : 8 * j - rot / 2;
-        other = INTER || !turned ? l : first ? l + rot / 16 : l - rot / 16;
-        sign = first ? -1.f : 1.f;
-    }
-};
-
-template <int GL>
-__device__ __forceinline__ float sum_over_head(float v) {
-#pragma unroll
-    for (int o = GL / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-
-// Cosine and (signed) sine of each of a lane's entries.
-template <int GL, bool INTER>
-__device__ __forceinline__ void angles(const RopeArgs& p, const RopeLane<GL, INTER>& ln, int pos, bool known, float (&c)[8], float (&s)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { c[i] = 1.f; s[i] = 0.f; }
-    if (!ln.turned || !known) return;
-    const float* cr = p.cos_ + (int64_t)pos * (p.rot / 2) + ln.at;
-    const float* sr = p.sin_ + (int64_t)pos * (p.rot / 2) + ln.at;
-    if constexpr (INTER) {
-        const f32x4 cv = *(const f32x4*)cr, sv = *(const f32x4*)sr;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { c[i] = cv[i / 2]; s[i] = i & 1 ? sv[i / 2] : -sv[i / 2]; }
-    } else {
-        const f32x4 c0 = *(const f32x4*)cr, c1 = *(const f32x4*)(cr + 4), s0 = *(const f32x4*)sr, s1 = *(const f32x4*)(sr + 4);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { c[i] = i < 4 ? c0[i & 3] : c1[i & 3]; s[i] = ln.sign * (i < 4 ? s0[i & 3] : s1[i & 3]); }
-    }
-}
-
-// The other entries of this lane's pairs.
-template <int GL, bool INTER>
-__device__ __forceinline__ void others(const RopeLane<GL, INTER>& ln, u32x4 raw, float (&o)[8]) {
-    if constexpr (INTER) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = raw[i] >> 16 | raw[i] << 16;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = __shfl(raw[i], ln.other);
-    }
-    unpack8(raw, o);
-}
-
-template <int GL, bool INTER>
-__device__ __forceinline__ u32x4 gamma_of(const lora_bf16* g, const RopeLane<GL, INTER>& ln) {
-    u32x4 v = u32x4{0u, 0u, 0u, 0u};
-    if (ln.active) v = *(const u32x4*)(g + 8 * ln.j);
-    return v;
-}
-
-// A wave's row is done in passes of 64 / GL heads, first the queries' passes, then the keys'; part i of the row takes passes i, i + parts, ..
-template <int GL>
-struct RopePasses {
-    static constexpr int HEADS = 64 / GL;
-    int of_q, all;
-    // first of the keys' passes that part `part` takes
-    __device__ __forceinline__ int first_k(int part, int parts) const { const int r = (part - of_q) % parts; return r < 0 ? r + parts : r; }
-    __host__ __device__ RopePasses(int H, int G) : of_q((H + HEADS - 1) / HEADS), all((H + HEADS - 1) / HEADS + (G + HEADS - 1) / HEADS) {}
-};
 
 template <int GL, bool INTER>
 __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
@@ -279,16 +203,6 @@ static int rope_parts(int64_t M, int H, int G, bool backward) {
     const int64_t want = std::max((16 * kComputeUnits + M - 1) / std::max<int64_t>(M, 1), (int64_t)(backward ? (all + 2) / 4 | 1 : 1));
     return (int)std::min<int64_t>(want, all);
 }
-template <class F>
-static auto with_lanes(int D, F&& f) {
-    if (D <= 64) return f(std::integral_constant<int, 8>{});
-    if (D <= 128) return f(std::integral_constant<int, 16>{});
-    return f(std::integral_constant<int, 32>{});
-}
-
-template <class F>
-static hipError_t with_pairs(bool interleaved, F&& f) { return interleaved ? f(std::true_type{}) : f(std::false_type{}); }
-
 hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st) {
     return with_lanes(a.D, [&](auto gl) {
         a.parts = rope_parts<gl()>(a.M, a.H, a.G, false);

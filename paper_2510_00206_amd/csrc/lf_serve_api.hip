@@ -35,11 +35,13 @@ lora_status check_rope(int64_t M, int32_t H, int32_t G, int32_t D, int32_t rot, 
 
 lora_status paged(const lora_kv_cache* c, PagedCache& out) {
     if (!c || !c->k || !c->v || (c->fp8 && (!c->k_exp || !c->v_exp))) return LORA_ERR_NULL;
+    const int form = !c->fp8 ? kCacheBf16 : c->fp8 == LORA_KV_FP4 ? kCacheFp4 : kCacheFp8;
     if (c->pages < 1 || c->heads < 1 || c->dim < 1 || c->page < 1) return LORA_ERR_SHAPE;
     if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1)) || c->heads > 1024 || c->pages >= (1ll << 31) || (c->dim & 15) || c->dim > 256)
         return LORA_ERR_UNSUPPORTED;
+    if (form == kCacheFp4 && (c->dim & 31)) return LORA_ERR_UNSUPPORTED;
     if (misaligned(c->k) || misaligned(c->v)) return LORA_ERR_ALIGN;
-    out = PagedCache{c->k, c->v, c->k_exp, c->v_exp, c->pages, __builtin_ctz((unsigned)c->page), c->heads, c->dim, c->fp8 != 0};
+    out = PagedCache{c->k, c->v, c->k_exp, c->v_exp, c->pages, __builtin_ctz((unsigned)c->page), c->heads, c->dim, form};
     return LORA_OK;
 }
 
@@ -59,6 +61,14 @@ lora_status cache_copy(const lora_kv_cache* cache, const void* k, const void* v,
     a.ldk = ldk;
     a.ldv = ldv;
     a.M = M;
+    return LORA_OK;
+}
+
+lora_status check_weights(const void* W, const void* codes, const void* exps, int64_t N, int64_t K) {
+    if (N <= 0 || K <= 0 || N >= (1ll << 31) || K >= (1ll << 31)) return LORA_ERR_SHAPE;
+    if ((N & 63) || (K & 63) || N > (1 << 22) || K > (1 << 22)) return LORA_ERR_UNSUPPORTED;
+    if (!W || !codes || !exps) return LORA_ERR_NULL;
+    if (misaligned(W) || misaligned(codes) || misaligned(exps)) return LORA_ERR_ALIGN;
     return LORA_OK;
 }
 
@@ -134,6 +144,65 @@ lora_status lora_qk_norm_rope_bwd(const lora_bf16* q, const lora_bf16* k, const 
                rot, (int)positions, 1, eps};
     const RopeFinalizeArgs f{(const float*)workspace, dgamma_q, dgamma_k, rope_blocks(M, H, G, D), D, accumulate != 0};
     return done(launch_rope_bwd(a, interleaved != 0, f, (hipStream_t)stream));
+}
+
+lora_status lora_weights_write(const lora_bf16* W, int64_t N, int64_t K, uint8_t* codes, uint8_t* exps, lora_stream stream) {
+    const lora_status st = check_weights(W, codes, exps, N, K);
+    return st != LORA_OK ? st : done(launch_weights_write(WeightsArgs{(lora_bf16*)W, codes, exps, N * K}, (hipStream_t)stream));
+}
+
+lora_status lora_weights_read(const uint8_t* codes, const uint8_t* exps, int64_t N, int64_t K, lora_bf16* W, lora_stream stream) {
+    const lora_status st = check_weights(W, codes, exps, N, K);
+    return st != LORA_OK ? st : done(launch_weights_read(WeightsArgs{W, (uint8_t*)codes, (uint8_t*)exps, N * K}, (hipStream_t)stream));
+}
+
+lora_status lora_requests_quantised_fwd(const lora_bf16* X, const uint8_t* codes, const uint8_t* exps, const lora_bf16* A, const lora_bf16* B,
+                                        const int32_t* ids, const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P,
+                                        lora_bf16* Y, lora_bf16* S, lora_stream stream) {
+    if (M < 0 || K <= 0 || N <= 0 || M >= (1ll << 31) || K >= (1ll << 31) || N >= (1ll << 31) || P < 0 || P >= (1ll << 31)) return LORA_ERR_SHAPE;
+    if ((K & 63) || (N & 63) || K > (1 << 22) || N > (1 << 22) || (P > 0 && !(r == 16 || r == 32 || r == 64)) || M >= (1 << 21)) return LORA_ERR_UNSUPPORTED;
+    if (!codes || !exps || (M > 0 && (!X || !Y)) || (P > 0 && (!A || !B || !s || (M > 0 && (!ids || !S))))) return LORA_ERR_NULL;
+    if (misaligned(X) || misaligned(codes) || misaligned(exps) || misaligned(Y)) return LORA_ERR_ALIGN;
+    if (P > 0 && (misaligned(A) || misaligned(B) || misaligned(S) || misaligned(ids, 4) || misaligned(ranks, 4) || misaligned(s, 4))) return LORA_ERR_ALIGN;
+    if (M == 0) return LORA_OK;
+    return done(launch_quantised_requests(
+        QuantisedRequestArgs{RequestArgs{X, nullptr, A, B, ids, ranks, s, Y, S, (int)M, (int)K, (int)N, r, (int)P}, codes, exps}, (hipStream_t)stream));
+}
+
+lora_status lora_kv_cache_append(const lora_kv_cache* cache, const lora_bf16* q, const lora_bf16* k, const lora_bf16* v, const lora_bf16* gamma_q,
+                                 const lora_bf16* gamma_k, const float* cos_table, const float* sin_table, const int32_t* pos, const int64_t* slots, int64_t M,
+                                 int32_t H, int32_t rot, int64_t positions, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, float eps, int interleaved,
+                                 lora_bf16* q_out, lora_stream stream) {
+    AppendArgs a{};
+    lora_status st = paged(cache, a.c);
+    if (st == LORA_OK) st = check_rope(M, H, a.c.heads, a.c.D, rot, positions, eps);
+    if (st != LORA_OK) return st;
+    if (!gamma_q != !gamma_k || (positions && (!cos_table || !sin_table)) || (M > 0 && (!q || !k || !v || !pos || !slots || !q_out))) return LORA_ERR_NULL;
+    if (bad_stride(ldq, H, a.c.D) || bad_stride(ldqo, H, a.c.D) || bad_stride(ldk, a.c.heads, a.c.D) || bad_stride(ldv, a.c.heads, a.c.D)) return LORA_ERR_SHAPE;
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(gamma_q) || misaligned(gamma_k) || misaligned(cos_table) || misaligned(sin_table) ||
+        misaligned(pos, 4) || misaligned(slots, 8) || misaligned(q_out))
+        return LORA_ERR_ALIGN;
+    if (M == 0) return LORA_OK;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.gamma_q = gamma_q;
+    a.gamma_k = gamma_k;
+    a.cos_ = cos_table;
+    a.sin_ = sin_table;
+    a.pos = pos;
+    a.slots = slots;
+    a.q_out = q_out;
+    a.ldq = ldq;
+    a.ldk = ldk;
+    a.ldv = ldv;
+    a.ldqo = ldqo;
+    a.M = M;
+    a.H = H;
+    a.rot = rot;
+    a.positions = (int)positions;
+    a.eps = eps;
+    return done(launch_append(a, interleaved != 0, (hipStream_t)stream));
 }
 
 lora_status lora_kv_cache_write(const lora_kv_cache* cache, const lora_bf16* k, const lora_bf16* v, int64_t ldk, int64_t ldv, const int64_t* slots,

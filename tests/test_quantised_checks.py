@@ -1,0 +1,96 @@
+"""The entry points around 4-bit weights and caches refuse bad arguments on the host, before anything is enqueued, with the documented status."""
+import ctypes as C
+import os
+
+import pytest
+
+P = C.c_void_p
+OK, NULL, SHAPE, ALIGN, PARAM, WORKSPACE, UNSUPPORTED = 0, 1, 2, 3, 4, 6, 7
+FP4 = -4
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2510_00206_amd import binding
+    if not os.path.exists(binding.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    assert binding.KV_FP4 == FP4
+    return binding.load_library()
+
+
+def _changed(good, **kw):
+    return list({**good, **kw}.values())
+
+
+def _cache(**kw):
+    from paper_2510_00206_amd import binding
+    good = dict(k=0x1000, v=0x1000, k_exp=0x1000, v_exp=0x1000, pages=8, page=16, heads=2, dim=64, fp8=FP4)
+    return C.byref(binding.CacheArrays(*_changed(good, **kw)))
+
+
+@pytest.mark.parametrize("name", ["lora_weights_write", "lora_weights_read"])
+def test_weights(lib, name):
+    p = P(0x1000)
+    keys = ("W", "N", "K", "codes", "exps") if name.endswith("write") else ("codes", "exps", "N", "K", "W")
+    good = {**{k: 64 if k in "NK" else p for k in keys}, "stream": None}
+    f = lambda **kw: getattr(lib, name)(*_changed(good, **kw))
+    for k in ("W", "codes", "exps"):
+        assert f(**{k: None}) == NULL, k
+        assert f(**{k: P(0x1008)}) == ALIGN, k
+    assert [f(N=0), f(K=0), f(N=-64), f(K=1 << 31), f(N=1 << 40)] == [SHAPE] * 5
+    assert [f(N=96), f(K=32), f(K=100), f(N=1 << 23), f(K=1 << 23)] == [UNSUPPORTED] * 5
+
+
+def test_layer(lib):
+    p = P(0x1000)
+    good = dict(X=p, codes=p, exps=p, A=p, B=p, ids=p, ranks=None, s=p, M=8, K=64, N=128, r=16, P=3, Y=p, S=p, stream=None)
+    f = lambda **kw: lib.lora_requests_quantised_fwd(*_changed(good, **kw))
+    assert f(M=0) == OK and f(M=0, X=None, ids=None, Y=None, S=None) == OK
+    none = dict(A=None, B=None, ids=None, s=None, S=None, P=0, r=0)
+    assert f(M=0, **none) == OK and f(**{**none, "X": None}) == NULL and f(**{**none, "Y": None}) == NULL and f(**{**none, "codes": None}) == NULL
+    for name in ("X", "codes", "exps", "A", "B", "ids", "s", "Y", "S"):
+        assert f(**{name: None}) == NULL, name
+    assert [f(M=-1), f(K=0), f(N=-64), f(P=-1), f(M=1 << 31), f(P=1 << 31)] == [SHAPE] * 6
+    assert [f(K=96), f(N=100), f(r=8), f(r=48), f(K=1 << 23), f(N=1 << 23), f(M=1 << 21)] == [UNSUPPORTED] * 7
+    for name in ("X", "codes", "exps", "A", "B", "Y", "S"):
+        assert f(**{name: P(0x1008)}) == ALIGN, name
+    assert f(ids=P(0x1002)) == ALIGN and f(ranks=P(0x1001)) == ALIGN and f(s=P(0x1002)) == ALIGN
+
+
+@pytest.mark.parametrize("fp8", [0, 1, FP4])
+def test_append(lib, fp8):
+    p, c = P(0x1000), _cache(fp8=fp8)
+    good = dict(cache=c, q=p, k=p, v=p, gq=p, gk=p, cos=p, sin=p, pos=p, slots=p, M=4, H=4, rot=64, positions=10, ldq=256, ldk=128, ldv=128, ldqo=256, eps=1e-6,
+                inter=0, qo=p, stream=None)
+    f = lambda **kw: lib.lora_kv_cache_append(*_changed(good, **kw))
+    assert f(M=0) == OK and f(M=0, q=None, k=None, v=None, pos=None, slots=None, qo=None, gq=None, gk=None) == OK
+    assert f(M=0, positions=0, cos=None, sin=None) == OK
+    for name in ("cache", "q", "k", "v", "gq", "gk", "cos", "sin", "pos", "slots", "qo"):
+        assert f(**{name: None}) == NULL, name
+    assert [f(M=-1), f(H=0), f(positions=-1), f(positions=1 << 31), f(ldq=248), f(ldk=120), f(ldv=132), f(ldqo=260)] == [SHAPE] * 8
+    assert [f(rot=8), f(rot=80), f(rot=40), f(H=1025), f(M=1 << 26)] == [UNSUPPORTED] * 5
+    assert [f(eps=0.0), f(eps=-1.0), f(eps=float("nan")), f(eps=float("inf"))] == [PARAM] * 4
+    for name in ("q", "k", "v", "gq", "gk", "cos", "sin", "qo"):
+        assert f(**{name: P(0x1008)}) == ALIGN, name
+    assert f(pos=P(0x1002)) == ALIGN and f(slots=P(0x1004)) == ALIGN
+    if fp8:
+        assert f(cache=_cache(fp8=fp8, k_exp=None)) == NULL and f(cache=_cache(fp8=fp8, v_exp=None)) == NULL
+    for bad in (dict(page=8), dict(page=48), dict(dim=72), dict(heads=1025)):
+        assert f(cache=_cache(fp8=fp8, **bad)) == UNSUPPORTED, bad
+
+
+def test_cache_in_4_bits(lib):
+    """Entries in 32s; everything else as for the other forms.  Any other number but 0 still is fp8."""
+    p = P(0x1000)
+    w = lambda c, M=4: lib.lora_kv_cache_write(c, p, p, 512, 512, p, M, None)
+    r = lambda c, M=4: lib.lora_kv_cache_read(c, p, M, p, p, 512, 512, None)
+    a = lambda c, T=4: lib.lora_paged_attn_fwd(p, c, p, p, p, T, 8, 2, 5, 1024, 5, 1024, 2, 80, 0.1, 0, p, p, 1 << 30, None)
+    for f in (w, r):
+        assert f(_cache(), 0) == OK and f(_cache(dim=96), 0) == OK and f(_cache(dim=80, fp8=1), 0) == OK and f(_cache(dim=80, fp8=4), 0) == OK
+        assert f(_cache(dim=80), 0) == UNSUPPORTED and f(_cache(dim=16), 0) == UNSUPPORTED and f(_cache(k_exp=None)) == NULL and f(_cache(v_exp=None)) == NULL
+        assert f(_cache(k=0x1008)) == ALIGN
+    assert a(_cache(), 0) == OK and a(_cache(dim=96)) == UNSUPPORTED and a(_cache(dim=80)) == UNSUPPORTED and a(_cache(v_exp=None)) == NULL
+    for dim in (64, 128):
+        one, other = (lib.lora_paged_attn_workspace_bytes(_cache(dim=dim, heads=8, fp8=form), 4, 32, 4, 1, 131072, 0) for form in (1, FP4))
+        assert one == other > 256
