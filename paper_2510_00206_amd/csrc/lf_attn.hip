@@ -564,17 +564,6 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
     }
 }
 
-// f(0), f(1), .., f(N - 1), each with its number as a constant.
-template <int N, int I = 0, class F>
-__device__ __forceinline__ void each(F&& f) {
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>{});
-        each<N, I + 1>(f);
-    }
-}
-// How many of `items`, spread over `slots`, come before slot n.
-constexpr int slots_before(int n, int items, int slots) { return n <= 0 ? 0 : n >= slots ? items : (n * items + slots - 1) / slots; }
-
 // ---- many rows --------------------------------------------------------------------------------------
 // Two workgroups of four waves on a compute unit, 32 rows to a wave, so that what is read of a tile in LDS serves two blocks of rows.  The scores of
 // tile n + 1, the softmax of tile n and the values of tile n - 1 are one stream of instructions, in which the vector ones stand between the matrix

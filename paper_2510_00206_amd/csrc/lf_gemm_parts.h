@@ -1,6 +1,8 @@
 // Device-side pieces that the GEMM kernels of operations (2) and (5) share (lf_gemm.hip: the large tiles;
 // lf_gemm_ring.hip: the small ones): workgroup -> tile map, global -> LDS slab copies, waits.
 #pragma once
+#include <type_traits>
+
 #include "lf_device.h"
 
 namespace lf {
@@ -65,6 +67,17 @@ __device__ __forceinline__ void wait_slab_loads() { asm volatile("s_waitcnt vmcn
 // all copies but the N issued last have landed (loads of a wave complete in order; only valid while no stores
 // of the wave are outstanding)
 template <int N> __device__ __forceinline__ void wait_slab_loads_but() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+
+// f(0), f(1), .., f(N - 1), each with its number as a constant.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void each(F&& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
+// How many of `items`, spread over `slots`, come before slot n.
+constexpr int slots_before(int n, int items, int slots) { return n <= 0 ? 0 : n >= slots ? items : (n * items + slots - 1) / slots; }
 
 // ---- the MFMA ------------------------------------------------------------------------------------
 #define LF_MFMA(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16((a), (b), (c), 0, 0, 0)

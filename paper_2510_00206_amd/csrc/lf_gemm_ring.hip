@@ -39,6 +39,7 @@ struct Ring {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NS = NS_, TW = TW_, OW = OW_, CW = TW + OW, D = D_;
     static constexpr int NW = WM * WN, THREADS = 64 * NW;             // waves and threads that compute
     static constexpr int MI = TM / WM / 16, NI = TN / WN / 16;        // 16x16 blocks per wave
+    static constexpr int EVERY = 1, HELD = 0;                         // (a wave forms the whole term of its rows, by itself: lf_request_term.h)
     static constexpr int DEPTH = D * BK, SUBS = 2 * D;                // contraction elements and sub-steps of 32 to a stage
     static constexpr int ROWB = DEPTH * 2;                            // bytes of a row in a row-operand slab
     static constexpr int STAGE = (TM + TN) * ROWB;

@@ -31,9 +31,10 @@ struct RequestList {                                          // of a wave
     int id[ROWS];                                             // adapter of each row, -1: none
     u32x2 unit[2 * ROWS];                                     // adapter; its rank, (8 bits on) the first of the unit's columns, (16 bits on) blocks with rows of it
 };
+// EVERY > 1: the term is shared out over so many waves with the same rows, this one taking every EVERY-th step from `first` on.
 template <class C>
 struct RequestTerm {
-    static constexpr int MI = C::MI, NI = C::NI, ROWS = MI * 16;
+    static constexpr int MI = C::MI, NI = C::NI, ROWS = MI * 16, EVERY = C::EVERY;
     static_assert(ROWS <= 64, "a lane for every row");
     // what the registers hold beside the accumulators, S and some forty others (LATE: and the fragments of the base product and the term's own
     // accumulators), with two workgroups on a compute unit where the rings allow two (32 x 32 tiles are taken while each has one for itself)
@@ -41,12 +42,13 @@ struct RequestTerm {
     static constexpr int FRAGS = (C::AHEAD ? 2 * C::SUBS : 2) * (MI + NI) * 4 + MI * NI * 4;
     static constexpr int fit(int beside) { return (HOLD - MI * NI * 4 - MI * 8 - 40 - beside) / (NI * 4 + 2); }
     static constexpr bool LATE = fit(FRAGS) >= 4;
-    static constexpr int FIT = fit(LATE ? FRAGS : 0), DEPTH = FIT < 1 ? 1 : FIT > 8 ? 8 : FIT;
+    static constexpr int FIT = fit(LATE ? FRAGS : C::HELD), DEPTH = FIT < 1 ? 1 : FIT > 8 ? 8 : FIT;
 
     const RingRequestArgs& p;
     const RequestList<C>& list;
     const lora_bf16* s0;
-    int n = 0, steps = 0, col0;                               // units, steps; first column of the wave
+    int n = 0, steps = 0, col0;                               // units, steps of this wave; first column of the wave
+    int first;
     int id[MI];
     int row0, rows;                                           // first row of the wave; of the tile
     uint32_t boff[NI];                                        // (32-bit offsets within an adapter: N <= 2^22, r <= 64)
@@ -54,8 +56,9 @@ struct RequestTerm {
     u32x4 b[DEPTH][NI];
     u32x2 e[DEPTH];                                           // the lane's unit
 
-    __device__ __forceinline__ RequestTerm(const RingRequestArgs& args, const RowTile& rt, int c0, int wm, int wn, RequestList<C>& out)
-        : p(args), list(out), s0(args.ltok + (int64_t)rt.row_start * args.lr), col0(c0 + wn * NI * 16), row0(wm * ROWS), rows(rt.rows) {
+    __device__ __forceinline__ RequestTerm(const RingRequestArgs& args, const RowTile& rt, int c0, int wm, int wn, RequestList<C>& out,
+                                           int from = 0)
+        : p(args), list(out), s0(args.ltok + (int64_t)rt.row_start * args.lr), col0(c0 + wn * NI * 16), first(from), row0(wm * ROWS), rows(rt.rows) {
         const int l = threadIdx.x & 63, q = l >> 4, width = p.lr == 16 ? 16 : 32;
         const int row = wm * ROWS + l;
         int of = p.ids[rt.row_start + min(row, rt.rows - 1)];
@@ -83,6 +86,7 @@ struct RequestTerm {
             if (more) out.unit[at + 1] = u32x2{(uint32_t)of, (uint32_t)rank | 32u << 8 | blocks << 16};
         }
         steps = width == 16 ? (n + 1) / 2 : n;
+        if constexpr (EVERY > 1) steps = max(steps - first + EVERY - 1, 0) / EVERY;
         asm volatile("" ::: "memory");                        // (LDS operations of a wave complete in order)
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
@@ -105,6 +109,7 @@ struct RequestTerm {
 
     // A lane's unit in a step (past the last one: that one, with nothing of it), and how many entries of its eight the adapter has there.
     __device__ __forceinline__ u32x2 unit_of(int step) const {
+        if constexpr (EVERY > 1) step = first + step * EVERY;
         const int u = p.lr == 16 ? 2 * step + ((threadIdx.x & 63) >> 5) : step;
         u32x2 v = list.unit[min(u, n - 1)];
         if (u >= n) v.y = 0u;
@@ -196,6 +201,7 @@ struct RequestTerm {
         ring_mfma_done<MI, NI>(acc);
 #pragma unroll 1
         for (int u = 0; u < n; ++u) {
+            if (EVERY > 1 && (p.lr == 16 ? u / 2 : u) % EVERY != first) continue;
             const u32x2 unit = list.unit[u];
             const int g = (int)unit.x, k0 = column_of(unit.y);
 #pragma unroll 1
