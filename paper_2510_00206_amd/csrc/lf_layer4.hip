@@ -20,16 +20,6 @@ struct LayerArgs {
     const uint8_t* codes; const uint8_t* exps;
 };
 
-// A lane's 32 codes and their power of two: row n of W, entries k .. k + 31.
-__device__ __forceinline__ void load_codes(const LayerArgs& p, int n, int k, u32x4& code, uint32_t& e) {
-    code = *(const u32x4*)(p.codes + (int64_t)n * (p.t.KC / 2) + k / 2);
-    e = p.exps[(int64_t)n * (p.t.KC / 32) + k / 32];
-}
-
-// A lane's place in the contraction: entries 32 q .. of a block; in the half block at the end, if there is one, 16 q + 8 j .. of two steps, of which its load
-// holds one half.
-__device__ __forceinline__ int entry_of(int b, int whole, int q) { return kBlock * b + (b < whole ? 32 * q : 32 * (q >> 1)); }
-
 // A matrix instruction from assembly with the accumulator tied in place (the compiler's own moved accumulators between registers).  FROM_VALU: its operands may come
 // straight from the vector ALU, which takes two wait states.
 template <bool FROM_VALU>
@@ -44,89 +34,170 @@ __device__ __forceinline__ void copy4_to_lds(const char* biased_base, uint32_t l
     asm volatile("global_load_lds_dword %0, %1 offset:%2" :: "v"(lane_byte_off), "s"(biased_base), "n"(IMM) : "memory");
 }
 
+// Copies of rows of 16-byte chunks, N of 1 KB, to `to`; off: biased (kCopyBias, pass_imm).
+template <int N, int I = 0>
+__device__ __forceinline__ void copy_rows(const char* biased, const uint32_t (&off)[N], uint32_t to) {
+    if constexpr (I < N) {
+        copy16_to_lds<pass_imm(N, I), I == 0>(biased, off[I], to + N / 2 * 1024);
+        copy_rows<N, I + 1>(biased, off, to);
+    }
+}
+// Position of 16-byte chunk ch of a row: of X (256 bytes), where the 16 rows of a fragment need 16 positions; of codes (64 bytes), where four rows share 256 bytes.
+__device__ __forceinline__ int x_chunk(int row, int ch) { return ch ^ (row & 15); }
+__device__ __forceinline__ int code_chunk(int row, int ch) { return ch ^ (row >> 2 & 3); }
+
+// What one wave brings of a block into LDS, and how: XC x 4 rows of X to `x`; CC x 16 rows of codes from row c0 + first on to `part`, behind them their exponents (four bytes a
+// row, for 64 lanes) and, SPLIT, the four bytes behind those: where rows are not whole blocks every other row's block starts in the middle of four bytes.
+template <int XC, int CC, bool SPLIT>
+struct BlockCopies {
+    static constexpr int N = XC + CC + (SPLIT ? 2 : 1), RW = 16 * CC, PART = RW * (kBlock / 2) + 512;
+    static constexpr int AT = (CC - CC / 2) * 1024;            // M0 stands in the middle of the codes: the exponents' immediates count from there
+    const LayerArgs& p;
+    int x_row, x_rows, first, c0, whole;
+    uint32_t xo[XC], co[CC], eo, left;
+    const char* x;
+    const char* codes;
+    const char* exps;
+
+    // x_first: of the wave's rows of X in the tile; code_first: of its rows of codes
+    __device__ __forceinline__ BlockCopies(const LayerArgs& args, const RowTile& rt, int tile_c0, int x_first, int code_first)
+        : p(args), x_row(x_first), x_rows(rt.rows), first(code_first), c0(tile_c0), whole(args.t.KC / kBlock) {
+        const int l = threadIdx.x & 63, K = p.t.KC;
+        form(kBlock / 2);
+        eo = (uint32_t)min(first + l % RW, p.t.NC - 1 - c0) * (uint32_t)(K / 32) + kCopyBias - AT;
+        x = (const char*)(p.t.tok + (int64_t)rt.row_start * K) - kCopyBias;
+        codes = (const char*)p.codes + (int64_t)c0 * (K / 2) - kCopyBias;
+        exps = (const char*)p.exps + (int64_t)c0 * (K / 32) - kCopyBias;
+        left = (uint32_t)min((int64_t)(p.t.NC - c0) * (K / 32), (int64_t)1 << 30);      // to the array's end, from the tile's first row
+    }
+    __device__ __forceinline__ void form(int bytes) {          // valid bytes of a row of codes
+        const int l = threadIdx.x & 63, K = p.t.KC;
+#pragma unroll
+        for (int i = 0; i < XC; ++i) {
+            const int row = x_row + 4 * i + l / 16, ch = min(x_chunk(row, l % 16), bytes / 4 - 1);
+            xo[i] = ((uint32_t)min(row, x_rows - 1) * (uint32_t)K + 8 * ch) * 2 + kCopyBias - pass_imm(XC, i);
+        }
+#pragma unroll
+        for (int i = 0; i < CC; ++i) {
+            const int row = first + 16 * i + l / 4, ch = min(code_chunk(row, l % 4), bytes / 16 - 1);
+            co[i] = (uint32_t)min(row, p.t.NC - 1 - c0) * (uint32_t)(K / 2) + 16 * ch + kCopyBias - pass_imm(CC, i);
+        }
+    }
+    __device__ __forceinline__ void block(int b, uint32_t x_to, uint32_t part_to) {
+        if (b >= whole) form(kBlock / 4);
+        copy_rows<XC>(x + (int64_t)b * (2 * kBlock), xo, __builtin_amdgcn_readfirstlane(x_to));
+        copy_rows<CC>(codes + (int64_t)b * (kBlock / 2), co, __builtin_amdgcn_readfirstlane(part_to));
+        const char* e = exps + (int64_t)b * (kBlock / 32);
+        if constexpr (SPLIT) {
+            // the offsets are even, from an array whose start is a multiple of 16, as is the tile's first row
+            const uint32_t at = eo - (kCopyBias - AT) + b * (kBlock / 32), down = at & 2u, behind = min(at - down + 4, left - 4);
+            copy4_to_lds<AT>(e, eo - down);
+            copy4_to_lds<AT + 256>(exps, behind + kCopyBias - AT - 256);
+        } else {
+            copy4_to_lds<AT>(e, eo);
+        }
+    }
+};
+// Byte of a lane's exponent behind the codes of its part, row r of it (c = r & 15); half: of the half block at the end.
+__device__ __forceinline__ int exp_byte(bool split, int r, int c, int q) { return 4 * r + (split && (c & 1) ? (q < 2 ? 2 + q : 256 - 2 + q) : q); }
+__device__ __forceinline__ int half_exp_byte(int r, int c, int q) { return 4 * r + 2 * (c & 1) + (q >> 1); }
+
 // ---- few rows ---------------------------------------------------------------------------------------
-// Bound by the reading of the weights.  A workgroup has NI x 16 columns and MI x 16 rows, its NW waves every NW-th block of the contraction, U blocks under way
-// at once; the adapters' term is formed by TW waves of its own beside them, which share its steps.  Sums of the waves are added in LDS in a fixed order.
-template <int MI_, int NI_, int NW_, int TW_, int U_>
+// Bound by the reading of the weights.  A workgroup has up to 16 rows (of which it brings 4 XC) and NI x 16 columns, its NW waves every NW-th block of the contraction, which each brings into a ring of
+// its own of D blocks, with no barrier; the adapters' term is formed by TW waves of its own beside them, which share its steps.  Sums of the waves are added in LDS
+// in a fixed order.
+template <int XC_, int NI_, int NW_, int TW_, int D_>
 struct FewLayer {
-    static constexpr int MI = MI_, NI = NI_, NW = NW_, TW = TW_, U = U_, TM = 16 * MI, TN = 16 * NI;
+    static constexpr int XC = XC_, NI = NI_, NW = NW_, TW = TW_, D = D_, TN = 16 * NI;
     struct Term {                      // of one wave
-        static constexpr int MI = MI_, NI = NI_, NW = NW_, CW = TW_, LDS = 160 * 1024, TN = 16 * NI_, SUBS = 0, EVERY = TW_, HELD = 0;
+        static constexpr int MI = 1, NI = NI_, NW = NW_, CW = TW_, LDS = 160 * 1024, TN = 16 * NI_, SUBS = 0, EVERY = TW_, HELD = 0;
         static constexpr bool AHEAD = false;
     };
-    static constexpr int SUMS = (NW + TW) * MI * NI * 1024, LDS = SUMS + TW * (int)sizeof(RequestList<Term>);
-    static_assert(LDS <= 160 * 1024, "a compute unit's LDS");
+    static constexpr int SLOT = XC * 1024 + BlockCopies<XC, NI, true>::PART;
+    static constexpr int RING = NW * D * SLOT, SUMS = (NW + TW) * NI * 1024, BODY = RING > SUMS ? RING : SUMS;
+    static constexpr int LDS = BODY + TW * (int)sizeof(RequestList<Term>);
+    static_assert((XC + NI + 2) * (D - 1) < 64 && LDS <= 160 * 1024, "the wait counter; a compute unit's LDS");
 };
+
+template <class C, bool SPLIT>
+__device__ __forceinline__ void few_products(const LayerArgs& p, const RowTile& rt, int c0, int w, char* ring, f32x4 (&acc)[1][C::NI]) {
+    constexpr int NI = C::NI, D = C::D;
+    using Copies = BlockCopies<C::XC, NI, SPLIT>;
+    const int l = threadIdx.x & 63, c = l & 15, q = l >> 4, blocks = (p.t.KC + kBlock - 1) / kBlock;
+    Copies copies(p, rt, c0, 0, 0);
+    const uint32_t lds = lds_addr_of(ring);
+    const int xr = min(c, 4 * C::XC - 1);                      // (rows past those there are: results that are not stored)
+    auto ask = [&](int b, int slot) {
+        if (b < blocks) copies.block(b, lds + slot * C::SLOT, lds + slot * C::SLOT + C::XC * 1024);
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d) ask(w + C::NW * d, d);
+    int slot = 0;
+    for (int b = w; b < blocks; b += C::NW) {
+        if (b + C::NW * (D - 1) < blocks) wait_slab_loads_but<Copies::N*(D - 1)>();
+        else wait_slab_loads();
+        const char* st = ring + slot * C::SLOT;
+        const char* part = st + C::XC * 1024;
+        if (!SPLIT || b < copies.whole) {
+            bf16x8 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = __builtin_bit_cast(bf16x8, *(const u32x4*)(st + xr * 256 + (x_chunk(xr, 4 * q + j) << 4)));
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) {
+                const u32x4 cd = *(const u32x4*)(part + (16 * ni + c) * 64 + (code_chunk(c, q) << 4));
+                const float sc = exp2_of_biased(*(const uint8_t*)(part + Copies::RW * 64 + exp_byte(SPLIT, 16 * ni + c, c, q)));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[0][ni] = LF_MFMA(from_fp4(cd[j], sc), x[j], acc[0][ni]);
+            }
+        } else {                                               // half a block, in two steps: 16 entries of each row to a lane
+            bf16x8 x[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) x[j] = __builtin_bit_cast(bf16x8, *(const u32x4*)(st + xr * 256 + (x_chunk(xr, 2 * q + j) << 4)));
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) {
+                const u32x4 cd = *(const u32x4*)(part + (16 * ni + c) * 64 + (code_chunk(c, q >> 1) << 4));
+                const float sc = exp2_of_biased(*(const uint8_t*)(part + Copies::RW * 64 + half_exp_byte(16 * ni + c, c, q)));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[0][ni] = LF_MFMA(from_fp4(q & 1 ? cd[2 + j] : cd[j], sc), x[j], acc[0][ni]);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the block is read: its place is free)
+        ask(b + C::NW * D, slot);
+        slot = slot + 1 == D ? 0 : slot + 1;
+    }
+}
 
 template <class C, bool TERM>
 __global__ void __launch_bounds__(64 * (C::NW + (TERM ? C::TW : 0))) layer_few_kernel(LayerArgs p) {
-    constexpr int MI = C::MI, NI = C::NI, NW = C::NW, U = C::U, WAVES = NW + (TERM ? C::TW : 0);
+    constexpr int NI = C::NI, NW = C::NW, WAVES = NW + (TERM ? C::TW : 0);
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = l & 15, q = l >> 4;
-    const int tn = (int)blockIdx.x % p.t.tiles_n, tm = (int)blockIdx.x / p.t.tiles_n;
-    const int c0 = tn * C::TN, K = p.t.KC;
+    const int c0 = (int)blockIdx.x % p.t.tiles_n * C::TN;
     RowTile rt{};
-    rt.row_start = p.t.row_lo + tm * C::TM;
-    rt.rows = min(C::TM, p.t.row_hi - rt.row_start);
-    f32x4* sums = (f32x4*)smem;                                // [wave][mi][ni][lane]
-    f32x4 acc[MI][NI];
+    rt.row_start = p.t.row_lo + (int)blockIdx.x / p.t.tiles_n * 16;
+    rt.rows = min(16, p.t.row_hi - rt.row_start);
+    f32x4 acc[1][NI];
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int ni = 0; ni < NI; ++ni) acc[0][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (TERM && w >= NW) {
         using T = typename C::Term;
-        RequestTerm<T> term(p.t, rt, c0, 0, 0, ((RequestList<T>*)(smem + C::SUMS))[w - NW], w - NW);
+        RequestTerm<T> term(p.t, rt, c0, 0, 0, ((RequestList<T>*)(smem + C::BODY))[w - NW], w - NW);
         term.form(acc);
+    } else if (p.t.KC % kBlock) {
+        few_products<C, true>(p, rt, c0, w, smem + w * C::D * C::SLOT, acc);
     } else {
-        const lora_bf16* x[MI];
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi) x[mi] = p.t.tok + (int64_t)(rt.row_start + min(16 * mi + c, rt.rows - 1)) * K;
-        const int whole = K / kBlock, blocks = (K + kBlock - 1) / kBlock;
-        for (int b0 = w; b0 < blocks; b0 += NW * U) {
-            u32x4 code[U][NI], xr[U][MI][4];
-            uint32_t e[U][NI];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int b = min(b0 + NW * u, blocks - 1), k = entry_of(b, whole, q), kx = b < whole ? k : kBlock * b + 16 * q;
-#pragma unroll
-                for (int ni = 0; ni < NI; ++ni) load_codes(p, c0 + 16 * ni + c, k, code[u][ni], e[u][ni]);
-#pragma unroll
-                for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) xr[u][mi][j] = *(const u32x4*)(x[mi] + kx + (b < whole ? 8 * j : 8 * (j & 1)));
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int b = b0 + NW * u;
-                if (b >= blocks) break;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (j == 2 && b >= whole) break;
-#pragma unroll
-                    for (int ni = 0; ni < NI; ++ni) {
-                        const uint32_t half = q & 1 ? code[u][ni][2 + (j & 1)] : code[u][ni][j & 1];
-                        const bf16x8 wf = from_fp4(b < whole ? code[u][ni][j] : half, exp2_of_biased(e[u][ni]));
-#pragma unroll
-                        for (int mi = 0; mi < MI; ++mi) acc[mi][ni] = LF_MFMA(wf, __builtin_bit_cast(bf16x8, xr[u][mi][j]), acc[mi][ni]);
-                    }
-                }
-            }
-        }
+        few_products<C, false>(p, rt, c0, w, smem + w * C::D * C::SLOT, acc);
     }
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni) sums[((w * MI + mi) * NI + ni) * 64 + l] = acc[mi][ni];
     __syncthreads();
-    for (int b = w; b < MI * NI; b += WAVES) {
-        const int mi = b / NI, ni = b % NI, row = 16 * mi + c;
-        f32x4 y = sums[b * 64 + l];
+    f32x4* sums = (f32x4*)smem;                                // [wave][ni][lane]
 #pragma unroll
-        for (int i = 1; i < WAVES; ++i) y += sums[(i * MI * NI + b) * 64 + l];
-        if (row < rt.rows)
-            *(u32x2*)(p.t.res + (int64_t)(rt.row_start + row) * p.t.NC + c0 + 16 * ni + 4 * q) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-    }
+    for (int ni = 0; ni < NI; ++ni) sums[(w * NI + ni) * 64 + l] = acc[0][ni];
+    __syncthreads();
+    if (w >= NI) return;
+    f32x4 y = sums[w * 64 + l];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) y += sums[(i * NI + w) * 64 + l];
+    if (c < rt.rows) *(u32x2*)(p.t.res + (int64_t)(rt.row_start + c) * p.t.NC + c0 + 16 * w + 4 * q) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
 }
 
 // ---- more rows --------------------------------------------------------------------------------------
@@ -138,9 +209,8 @@ template <int MI_, int NI_, int WM_, int WN_, int NS_, int CW_>
 struct RingLayer {
     static constexpr int MI = MI_, NI = NI_, WM = WM_, WN = WN_, NS = NS_, CW = CW_, NW = WM * WN, THREADS = 64 * NW;
     static constexpr int TM = 16 * MI * WM, TN = 16 * NI * WN;
-    // a block: X, then of every copying wave the codes of RW rows, their exponents (four bytes a row, for 64 rows), and the four bytes behind those
-    static constexpr int XB = TM * 2 * kBlock, RW = TN / CW, PART = RW * (kBlock / 2) + 512, STAGE = XB + CW * PART;
-    static constexpr int XC = XB / 1024 / CW, CC = RW / 16;                         // copies of a wave: of X, of codes (of exponents: one or two)
+    static constexpr int XB = TM * 2 * kBlock, XC = XB / 1024 / CW, RW = TN / CW, CC = RW / 16;     // a block's X, then the parts of the copying waves
+    static constexpr int PART = BlockCopies<XC, CC, true>::PART, STAGE = XB + CW * PART;
     static constexpr int OUT = TM * TN * 2;
     static constexpr int HALVES = (MI + 3) / 4;                                     // the term is formed for 64 rows of a wave at a time
     struct Term {
@@ -154,73 +224,25 @@ struct RingLayer {
     static_assert((XC + CC + 2) * (NS - 2) < 64, "... and of the wait counter");
     static_assert(NS >= 3 && LDS <= 160 * 1024, "a compute unit's LDS");
 };
-// Position of 16-byte chunk ch of a row: of X (256 bytes), where the 16 rows of a fragment need 16 positions; of codes (64 bytes), where four rows share 256 bytes.
-__device__ __forceinline__ int x_chunk(int row, int ch) { return ch ^ (row & 15); }
-__device__ __forceinline__ int code_chunk(int row, int ch) { return ch ^ (row >> 2 & 3); }
-
 // The copying waves.  Block b + NS - 1 goes where block b - 1 was, which every wave has left when it comes to the barrier in block b; behind that barrier block
-// b + 1 has landed.  Exponents: the aligned four bytes with the first of a row's block, and, where rows are not whole blocks (SPLIT), the four behind
-// them, since every other row's block starts in the middle.
-template <class C, int N, int I = 0>
-__device__ __forceinline__ void copy_rows(const char* biased, const uint32_t (&off)[N], uint32_t to) {
-    if constexpr (I < N) {
-        copy16_to_lds<pass_imm(N, I), I == 0>(biased, off[I], to + N / 2 * 1024);
-        copy_rows<C, N, I + 1>(biased, off, to);
-    }
-}
+// b + 1 has landed.
 template <class C, bool SPLIT>
 __device__ __forceinline__ void copying_wave(const LayerArgs& p, const RowTile& rt, int c0, int w, uint32_t lds) {
-    constexpr int NS = C::NS, N = C::XC + C::CC + (SPLIT ? 2 : 1);
-    const int l = threadIdx.x & 63, K = p.t.KC, whole = K / kBlock, blocks = (K + kBlock - 1) / kBlock;
-    uint32_t xo[C::XC], co[C::CC], eo;
-    auto form = [&](int bytes) {                               // valid bytes of a row of codes
-#pragma unroll
-        for (int i = 0; i < C::XC; ++i) {
-            const int row = (w * C::XC + i) * 4 + l / 16, ch = min(x_chunk(row, l % 16), bytes / 4 - 1);
-            xo[i] = ((uint32_t)min(row, rt.rows - 1) * (uint32_t)K + 8 * ch) * 2 + kCopyBias - pass_imm(C::XC, i);
-        }
-#pragma unroll
-        for (int i = 0; i < C::CC; ++i) {
-            const int row = w * C::RW + 16 * i + l / 4, ch = min(code_chunk(row, l % 4), bytes / 16 - 1);
-            co[i] = (uint32_t)min(row, p.t.NC - 1 - c0) * (uint32_t)(K / 2) + 16 * ch + kCopyBias - pass_imm(C::CC, i);
-        }
-    };
-    {
-        // (M0 stands in the middle of the codes: the exponents' immediates count from there)
-        constexpr int at = (C::CC - C::CC / 2) * 1024;
-        eo = (uint32_t)min(w * C::RW + l % C::RW, p.t.NC - 1 - c0) * (uint32_t)(K / 32) + kCopyBias - at;
-    }
-    const char* x = (const char*)(p.t.tok + (int64_t)rt.row_start * K) - kCopyBias;
-    const char* codes = (const char*)p.codes + (int64_t)c0 * (K / 2) - kCopyBias;
-    const char* exps = (const char*)p.exps + (int64_t)c0 * (K / 32) - kCopyBias;
-    // exponents to the array's end, from the tile's first row
-    const uint32_t left = (uint32_t)min((int64_t)(p.t.NC - c0) * (K / 32), (int64_t)1 << 30);
+    constexpr int NS = C::NS;
+    using Copies = BlockCopies<C::XC, C::CC, SPLIT>;
+    Copies copies(p, rt, c0, w * C::XC * 4, w * C::RW);
+    const int whole = copies.whole, blocks = (p.t.KC + kBlock - 1) / kBlock;
     auto block = [&](int b, int stage) {
-        if (b >= blocks) return;
-        if (b >= whole) form(kBlock / 4);
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + stage * C::STAGE + w * C::XC * 1024);
-        copy_rows<C, C::XC>(x + (int64_t)b * (2 * kBlock), xo, to);
-        copy_rows<C, C::CC>(codes + (int64_t)b * (kBlock / 2), co, __builtin_amdgcn_readfirstlane(lds + stage * C::STAGE + C::XB + w * C::PART));
-        constexpr int at = (C::CC - C::CC / 2) * 1024;
-        const char* e = exps + (int64_t)b * (kBlock / 32);
-        if constexpr (SPLIT) {
-            // the offsets are even, from an array whose start is a multiple of 16, as is the tile's first row
-            const uint32_t first = eo - (kCopyBias - at) + b * (kBlock / 32), down = first & 2u, behind = min(first - down + 4, left - 4);
-            copy4_to_lds<at>(e, eo - down);
-            copy4_to_lds<at + 256>(exps, behind + kCopyBias - at - 256);
-        } else {
-            copy4_to_lds<at>(e, eo);
-        }
+        if (b < blocks) copies.block(b, lds + stage * C::STAGE + w * C::XC * 1024, lds + stage * C::STAGE + C::XB + w * C::PART);
     };
-    form(kBlock / 2);
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s) block(s, s);
-    if (blocks >= NS - 1) wait_slab_loads_but<N*(NS - 2)>();
+    if (blocks >= NS - 1) wait_slab_loads_but<Copies::N*(NS - 2)>();
     else wait_slab_loads();
     asm volatile("s_barrier" ::: "memory");
     int stage = NS - 1;
     for (int b = 0; b < whole; ++b) {
-        if (b + NS - 1 <= blocks) wait_slab_loads_but<N*(NS - 3)>();
+        if (b + NS - 1 <= blocks) wait_slab_loads_but<Copies::N*(NS - 3)>();
         else wait_slab_loads();
         asm volatile("s_barrier" ::: "memory");
         block(b + NS - 1, stage);
@@ -280,13 +302,12 @@ __global__ void __launch_bounds__(C::THREADS + 64 * C::CW) layer_ring_kernel(Lay
         // rows 16 nb .. of the tile (nb = wn * NI + ni): the part of their copying wave, and the row in it
         auto part_of = [&](int stage, int ni) { return smem + stage * C::STAGE + C::XB + (wn * NI + ni) / (C::RW / 16) * C::PART; };
         auto row_of = [&](int ni) { return (wn * NI + ni) % (C::RW / 16) * 16 + c; };
-        const bool split = blocks > whole && (c & 1);           // this lane's rows' exponents start in the middle of four bytes
+        const bool split = blocks > whole;
         auto read_codes = [&](int stage, int ni) {
             coming[ni] = *(const u32x4*)(part_of(stage, ni) + row_of(ni) * 64 + (code_chunk(c, q) << 4));
         };
         auto read_exp = [&](int stage, int ni) {
-            const int byte = split ? (q < 2 ? 2 + q : 256 - 2 + q) : q;
-            e[ni] = *(const uint8_t*)(part_of(stage, ni) + C::RW * 64 + row_of(ni) * 4 + byte);
+            e[ni] = *(const uint8_t*)(part_of(stage, ni) + C::RW * 64 + exp_byte(split, row_of(ni), c, q));
         };
         auto arrive = [&](int ni) {
             code[ni] = coming[ni];
@@ -336,7 +357,7 @@ __global__ void __launch_bounds__(C::THREADS + 64 * C::CW) layer_ring_kernel(Lay
             for (int ni = 0; ni < NI; ++ni) {
                 const char* part = part_of(stage, ni);
                 const u32x4 cd = *(const u32x4*)(part + row_of(ni) * 64 + (code_chunk(c, q >> 1) << 4));
-                const float sc = exp2_of_biased(*(const uint8_t*)(part + C::RW * 64 + row_of(ni) * 4 + (split ? 2 : 0) + (q >> 1)));
+                const float sc = exp2_of_biased(*(const uint8_t*)(part + C::RW * 64 + half_exp_byte(row_of(ni), c, q)));
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const bf16x8 wh = from_fp4(q & 1 ? cd[2 + j] : cd[j], sc);
@@ -405,13 +426,33 @@ static hipError_t launch_layer(const LayerArgs& a, int tile_rows, int tile_colum
 
 template <class C>
 static hipError_t launch_few(const LayerArgs& a, hipStream_t st) {
-    if (a.t.P > 0) return launch_layer<layer_few_kernel<C, true>>(a, C::TM, C::TN, 64 * (C::NW + C::TW), C::LDS, st);
-    return launch_layer<layer_few_kernel<C, false>>(a, C::TM, C::TN, 64 * C::NW, C::LDS, st);
+    if (a.t.P > 0) return launch_layer<layer_few_kernel<C, true>>(a, 16, C::TN, 64 * (C::NW + C::TW), C::LDS, st);
+    return launch_layer<layer_few_kernel<C, false>>(a, 16, C::TN, 64 * C::NW, C::LDS, st);
 }
 template <class C>
 static hipError_t launch_ring(const LayerArgs& a, hipStream_t st) {
     if (a.t.P > 0) return launch_layer<layer_ring_kernel<C, true>>(a, C::TM, C::TN, C::THREADS + 64 * C::CW, C::LDS, st);
     return launch_layer<layer_ring_kernel<C, false>>(a, C::TM, C::TN, C::THREADS + 64 * C::CW, C::LDS, st);
+}
+
+// Rows and columns of a workgroup, and what a block of the contraction takes it, us, while there is one on a compute unit; 2.5 a round beside them (fitted to 1 - 2048
+// rows, K of 1024 - 14336, N of 1024 - 14336).  The first three are layer_few_kernel.
+struct LayerKind { int rows, columns; float block; };
+constexpr LayerKind kLayerKinds[] = {{16, 16, 0.085f}, {16, 32, 0.098f}, {16, 64, 0.152f}, {32, 64, 0.25f}, {64, 64, 0.30f}, {64, 128, 0.43f}, {64, 256, 0.62f},
+                                     {128, 256, 1.08f}};
+static int choose_kind(int M, int K, int N) {
+    int best = 0;
+    float least = 0.f;
+    for (int i = 0; i < (int)(sizeof(kLayerKinds) / sizeof(kLayerKinds[0])); ++i) {
+        const LayerKind& k = kLayerKinds[i];
+        const int64_t tiles = (int64_t)((M + k.rows - 1) / k.rows) * ((N + k.columns - 1) / k.columns);
+        const float us = (float)((tiles + kComputeUnits - 1) / kComputeUnits) * (2.5f + k.block * (float)K / kBlock);
+        if (i == 0 || us < least) {
+            least = us;
+            best = i;
+        }
+    }
+    return best;
 }
 
 hipError_t launch_quantised_requests(const QuantisedRequestArgs& a, hipStream_t st) {
@@ -431,15 +472,16 @@ hipError_t launch_quantised_requests(const QuantisedRequestArgs& a, hipStream_t 
     g.t.P = a.r.P;
     g.codes = a.codes;
     g.exps = a.exps;
-    int kind = a.r.M <= 16 ? 0 : a.r.M <= 32 ? 1 : a.r.M <= 64 ? 3 : a.r.M <= 256 ? 4 : 6;
+    int kind = choose_kind(a.r.M, a.r.K, a.r.N);
     switch (kind) {
-        case 0: return launch_few<FewLayer<1, 1, 8, 4, 2>>(g, st);
-        case 1: return launch_few<FewLayer<2, 1, 8, 4, 2>>(g, st);
-        case 2: return launch_ring<RingLayer<1, 2, 2, 2, 6, 1>>(g, st);        // 32 x 64
-        case 3: return launch_ring<RingLayer<2, 2, 2, 2, 7, 2>>(g, st);        // 64 x 64
-        case 4: return launch_ring<RingLayer<4, 2, 1, 4, 6, 2>>(g, st);        // 64 x 128
-        case 5: return launch_ring<RingLayer<4, 4, 1, 4, 4, 4>>(g, st);        // 64 x 256
-        default: return launch_ring<RingLayer<8, 4, 1, 4, 3, 4>>(g, st);       // 128 x 256
+        case 0: return a.r.M <= 4 ? launch_few<FewLayer<1, 1, 8, 4, 4>>(g, st) : launch_few<FewLayer<4, 1, 8, 4, 3>>(g, st);
+        case 1: return launch_few<FewLayer<4, 2, 8, 4, 2>>(g, st);
+        case 2: return launch_few<FewLayer<4, 4, 8, 4, 2>>(g, st);
+        case 3: return launch_ring<RingLayer<1, 2, 2, 2, 6, 1>>(g, st);
+        case 4: return launch_ring<RingLayer<2, 2, 2, 2, 7, 2>>(g, st);
+        case 5: return launch_ring<RingLayer<4, 2, 1, 4, 6, 2>>(g, st);
+        case 6: return launch_ring<RingLayer<4, 4, 1, 4, 4, 4>>(g, st);
+        default: return launch_ring<RingLayer<8, 4, 1, 4, 3, 4>>(g, st);
     }
 }
 
