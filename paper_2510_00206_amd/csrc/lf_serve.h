@@ -45,7 +45,7 @@ struct AppendArgs {
     const int32_t* pos; const int64_t* slots;
     lora_bf16* q_out;
     int64_t ldq, ldk, ldv, ldqo, M;
-    int H, rot, positions, parts;
+    int H, rot, positions, parts, kv_parts, kv_blocks;
     float eps;
 };
 

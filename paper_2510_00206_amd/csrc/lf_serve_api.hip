@@ -41,6 +41,7 @@ lora_status paged(const lora_kv_cache* c, PagedCache& out) {
         return LORA_ERR_UNSUPPORTED;
     if (form == kCacheFp4 && (c->dim & 31)) return LORA_ERR_UNSUPPORTED;
     if (misaligned(c->k) || misaligned(c->v)) return LORA_ERR_ALIGN;
+    if (form == kCacheFp4 && (misaligned(c->k_exp) || misaligned(c->v_exp))) return LORA_ERR_ALIGN;
     out = PagedCache{c->k, c->v, c->k_exp, c->v_exp, c->pages, __builtin_ctz((unsigned)c->page), c->heads, c->dim, form};
     return LORA_OK;
 }

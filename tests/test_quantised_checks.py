@@ -89,7 +89,7 @@ def test_cache_in_4_bits(lib):
     for f in (w, r):
         assert f(_cache(), 0) == OK and f(_cache(dim=96), 0) == OK and f(_cache(dim=80, fp8=1), 0) == OK and f(_cache(dim=80, fp8=4), 0) == OK
         assert f(_cache(dim=80), 0) == UNSUPPORTED and f(_cache(dim=16), 0) == UNSUPPORTED and f(_cache(k_exp=None)) == NULL and f(_cache(v_exp=None)) == NULL
-        assert f(_cache(k=0x1008)) == ALIGN
+        assert f(_cache(k=0x1008)) == ALIGN and f(_cache(k_exp=0x1004)) == ALIGN and f(_cache(v_exp=0x1008)) == ALIGN
     assert a(_cache(), 0) == OK and a(_cache(dim=96)) == UNSUPPORTED and a(_cache(dim=80)) == UNSUPPORTED and a(_cache(v_exp=None)) == NULL
     for dim in (64, 128):
         one, other = (lib.lora_paged_attn_workspace_bytes(_cache(dim=dim, heads=8, fp8=form), 4, 32, 4, 1, 131072, 0) for form in (1, FP4))
