@@ -8,6 +8,8 @@ adapter (lora_requests_fwd), queries and keys are normalised and turned (lora_qk
 (lora_kv_cache_write), the new tokens attend over it (lora_paged_attn_fwd), and the output projection takes the adapters again.  Prompts may come
 in chunks, beside requests that decode: what a step needs to know of them are arrays on the GPU, so that a step of fixed size can be
 captured in a HIP graph and replayed.
+Serving over 4 bits: the same block after quantise(): both projections over 4-bit weights (lora_requests_quantised_fwd), queries, keys and values from the
+projection to attention and the cache in one call (lora_kv_cache_append), which may be a 4-bit cache too.
 Training: the same projection and norm with the backward passes of the library."""
 import torch
 
@@ -34,10 +36,18 @@ class AttentionBlock:
         self.gamma_q, self.gamma_k = normal((dim,), 0.1, 1.0), normal((dim,), 0.1, 1.0)
         angle = torch.arange(positions, device=device)[:, None] * 10000.0 ** (-torch.arange(dim // 2, device=device) / (dim // 2))
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
+        self.four_bits = None
+
+    def quantise(self):
+        """Serve over 4-bit weights from here on; the bf16 ones stay for training.  -> the block"""
+        self.four_bits = binding.lora_weights_write(self.w_qkv), binding.lora_weights_write(self.w_out)
+        return self
 
     def serve(self, step, x):
         """x [tokens, hidden] of a Step -> the block's output [tokens, hidden]."""
         H, G, D = self.heads, self.kv_heads, self.dim
+        if self.four_bits:
+            return self._serve_four_bits(step, x)
         binding.lora_requests_fwd(x, self.w_qkv, self.a_qkv, self.b_qkv, step.adapters, self.scale, ranks=self.ranks, Y=step.qkv, S=step.s)
         q, k, v = (step.qkv[:, a * D:b * D].unflatten(1, (b - a, D)) for a, b in ((0, H), (H, H + G), (H + G, H + 2 * G)))
         binding.lora_qk_norm_rope_fwd(q, k, self.gamma_q, self.gamma_k, self.cos, self.sin, step.positions, q_out=q, k_out=k)
@@ -46,6 +56,17 @@ class AttentionBlock:
                                     workspace=step.workspace)
         return binding.lora_requests_fwd(step.mixed.flatten(1), self.w_out, self.a_out, self.b_out, step.adapters, self.scale, ranks=self.ranks,
                                          Y=step.out, S=step.s)[0]
+
+    def _serve_four_bits(self, step, x):
+        H, G, D = self.heads, self.kv_heads, self.dim
+        qkv, out = self.four_bits
+        binding.lora_requests_quantised_fwd(x, *qkv, self.a_qkv, self.b_qkv, step.adapters, self.scale, ranks=self.ranks, Y=step.qkv, S=step.s)
+        q, k, v = (step.qkv[:, a * D:b * D].unflatten(1, (b - a, D)) for a, b in ((0, H), (H, H + G), (H + G, H + 2 * G)))
+        binding.lora_kv_cache_append(step.cache, q, k, v, self.cos, self.sin, step.positions, step.slots, self.gamma_q, self.gamma_k, q_out=q)
+        binding.lora_paged_attn_fwd(q, step.cache, step.table, step.offsets, step.lengths, step.max_new, step.max_length, out=step.mixed,
+                                    workspace=step.workspace)
+        return binding.lora_requests_quantised_fwd(step.mixed.flatten(1), *out, self.a_out, self.b_out, step.adapters, self.scale, ranks=self.ranks,
+                                                   Y=step.out, S=step.s)[0]
 
     def train(self, x, positions, dq, dk, dv, adapter=0, dropout=0.1, seed=1):
         """One adapter's forward and backward of the projection with norm and rotation, for the gradients dq, dk, dv that attention returns.
@@ -92,23 +113,19 @@ class Step:
         self.table.copy_(rows([list(p) + [0] * (self.table.shape[1] - len(p)) for p in pages], I32))
 
 
-def main():
-    block = AttentionBlock(hidden=4096, heads=32, kv_heads=8, dim=128, rank=16, adapters=64)
-    requests, prompt, page, decode = 32, 1000, 16, 20
-    pages_each = -(-(prompt + decode) // page)
-    cache = binding.KVCache.empty(requests * pages_each, page, 8, 128, fp8=True)
+def serve(block, cache, label, requests=32, prompt=1000, decode=20):
+    """Prompts four at a time in chunks of 250, then decoding, one token of every request a step; prints the time of such a step."""
+    pages_each = cache.pages // requests
     pages = [list(range(i * pages_each, (i + 1) * pages_each)) for i in range(requests)]
     adapters = [i % 64 if i % 10 else -1 for i in range(requests)]
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
-    # prompts, four at a time in chunks of 250
     chunk = Step(block, cache, [250] * 4, prompt, pages_each)
     for first in range(0, requests, 4):
         for before in range(0, prompt, 250):
             ids = range(first, first + 4)
             chunk.plan([adapters[i] for i in ids], [pages[i] for i in ids], [before] * 4)
             block.serve(chunk, torch.randn((1000, 4096), generator=g, device="cuda").to(BF16))
-    # decoding, one token of every request a step
     step = Step(block, cache, [1] * requests, prompt + decode, pages_each)
     x = torch.randn((requests, 4096), generator=g, device="cuda").to(BF16)
     begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
@@ -118,8 +135,15 @@ def main():
         block.serve(step, x)
         end.record()
     torch.cuda.synchronize()
-    print(f"attention block, {requests} requests, {prompt + decode} tokens each, fp8 cache: {begin.elapsed_time(end) * 1e3:.0f} us a decode step; "
+    print(f"attention block, {requests} requests, {prompt + decode} tokens each, {label}: {begin.elapsed_time(end) * 1e3:.0f} us a decode step; "
           f"output finite: {bool(torch.isfinite(step.out).all())}")
+
+
+def main():
+    block = AttentionBlock(hidden=4096, heads=32, kv_heads=8, dim=128, rank=16, adapters=64)
+    pages = 32 * -(-1020 // 16)
+    serve(block, binding.KVCache.empty(pages, 16, 8, 128, fp8=True), "fp8 cache")
+    serve(block.quantise(), binding.KVCache.empty(pages, 16, 8, 128, fp4=True), "4-bit weights and cache")
 
 
 if __name__ == "__main__":

@@ -149,3 +149,37 @@ def test_large_offsets():
     assert torch.equal(W[-64:].cpu().to(F64), widened4(last, torch.full((64, K // 32), 127, dtype=torch.uint8)))
     c2, e2 = binding.lora_weights_write(W)
     assert torch.equal(binding.lora_weights_read(c2, e2)[-64:], W[-64:])
+
+
+@pytest.mark.parametrize("P", [0, 5])
+@pytest.mark.parametrize("M,K,N", [
+    (3, 192, 64), (4, 256, 4096),                          # 16 x 16 with four rows at most
+    (5, 256, 128), (16, 192, 4096),                        # 16 x 16
+    (16, 192, 6144), (20, 256, 4096),                      # 16 x 32
+    (30, 256, 4160), (16, 192, 8960),                      # 16 x 64
+    (48, 192, 6144), (96, 320, 4096), (40, 512, 8192),     # 32 x 64
+    (130, 192, 4160), (129, 256, 4160),                    # 64 x 64
+    (200, 192, 4160), (700, 256, 2112),                    # 64 x 128
+    (260, 256, 8192), (600, 192, 4096),                    # 64 x 256
+    (1300, 256, 4096), (2050, 320, 2112),                  # 128 x 256
+])
+def test_every_tile(M, K, N, P):
+    """Contractions that end with a block of 128 and with half a one, rows and columns past the last tile, with and without adapters."""
+    if P:
+        _check(_case(M, K, N, 16, P, "any", True, M + K), (M, K, N, P))
+    else:
+        test_without_adapters(M, K, N)
+
+
+def test_most_rows():
+    """2^21 - 1 rows, each an adapter of its own choice: the first and the last ones."""
+    M, K, N, r, P = (1 << 21) - 1, 64, 64, 16, 3
+    X, codes, exps, A, B, ids, s, _ = _case(600, K, N, r, P, "any", False, 5)
+    big = torch.zeros((M, K), dtype=BF16, device="cuda")
+    far = torch.full((M,), -1, dtype=torch.int32, device="cuda")
+    big[:300], big[-300:], far[:300], far[-300:] = X[:300].cuda(), X[300:].cuda(), ids[:300].cuda(), ids[300:].cuda()
+    Y, _ = binding.lora_requests_quantised_fwd(big, codes.cuda(), exps.cuda(), A.cuda(), B.cuda(), far, s.cuda())
+    ref, bound, _, _ = requests(X, widened4(codes, exps), A, B, ids, s, None)
+    within(Y[:300], ref[:300], bound[:300], "first rows")
+    within(Y[-300:], ref[300:], bound[300:], "last rows")
+    assert int((Y[300:-300] != 0).sum()) == 0
