@@ -18,6 +18,7 @@ constexpr int kBlock = 128;            // of the contraction, the last one may b
 struct LayerArgs {
     RingRequestArgs t;                 // tok X, ltok S, lout B, res Y
     const uint8_t* codes; const uint8_t* exps;
+    const lora_bf16* A; const float* s; lora_bf16* S;      // where the layer forms S by itself
 };
 
 // A matrix instruction from assembly with the accumulator tied in place (the compiler's own moved accumulators between registers).  FROM_VALU: its operands may come
@@ -167,8 +168,69 @@ __device__ __forceinline__ void few_products(const LayerArgs& p, const RowTile& 
     }
 }
 
-template <class C, bool TERM>
-__global__ void __launch_bounds__(64 * (C::NW + (TERM ? C::TW : 0))) layer_few_kernel(LayerArgs p) {
+// S and the term of a few rows in one go, in wave t of TW: each wave has its part of the adapter's columns, whose S it forms (in fp32, rounded to bf16 as where it is stored) and
+// multiplies with its part of B.  Every workgroup reads the rows' A for itself, row after row and four columns at a time, which has to be less than a launch of its own (launch_quantised_requests).
+template <class C>
+__device__ __forceinline__ void own_term(const LayerArgs& p, const RowTile& rt, int c0, int t, f32x4 (&acc)[1][C::NI]) {
+    const int l = threadIdx.x & 63, c = l & 15, q = l >> 4, K = p.t.KC, r = p.t.lr, own = r / C::TW;
+    for (int i = 0; i < rt.rows; ++i) {
+        const int64_t row = rt.row_start + i;
+        const int g = __builtin_amdgcn_readfirstlane(p.t.ids[row]);
+        const bool has = g >= 0 && g < p.t.P;
+        const int rank = has ? p.t.ranks ? max(min(__builtin_amdgcn_readfirstlane(p.t.ranks[g]), r), 0) : r : 0;
+        const float s = has ? p.s[g] : 0.f;
+        for (int j = t * own; j < (t + 1) * own; j += 4) {
+            u32x2 held = u32x2{0u, 0u};
+            if (j < rank) {
+                u32x2 b[C::NI][4];
+#pragma unroll
+                for (int ni = 0; ni < C::NI; ++ni)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        if (c == i) b[ni][n] = *(const u32x2*)(p.t.lout + ((int64_t)g * p.t.NC + c0 + 16 * ni + 4 * q + n) * r + j);
+                const lora_bf16* x = p.t.tok + row * K;
+                const lora_bf16* a = p.A + ((int64_t)g * r + j) * K;
+                float d[4] = {0.f, 0.f, 0.f, 0.f}, v[4];
+#pragma unroll 2
+                for (int k = 8 * l; k < K; k += 512) {
+                    float xf[8];
+                    unpack8(*(const u32x4*)(x + k), xf);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        float af[8];
+                        unpack8(*(const u32x4*)(a + (int64_t)u * K + k), af);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) d[u] += xf[e] * af[e];
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                    for (int o = 32; o > 0; o >>= 1) d[u] += __shfl_xor(d[u], o);
+                    v[u] = j + u < rank ? s * d[u] : 0.f;
+                }
+                held = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                if (c == i)
+#pragma unroll
+                    for (int ni = 0; ni < C::NI; ++ni)
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const uint32_t sh = u & 1 ? 0u : 16u;
+                                const float su = __builtin_bit_cast(float, held[u / 2] << sh & 0xFFFF0000u), bu = __builtin_bit_cast(float, b[ni][n][u / 2] << sh & 0xFFFF0000u);
+                                if (j + u < rank) acc[0][ni][n] += su * bu;
+                            }
+            }
+            if (c0 == 0 && l == 0) *(u32x2*)(p.S + row * r + j) = held;
+        }
+    }
+}
+
+enum class Few { plain, term, own };           // no adapters; their S from memory; formed here
+template <class C, Few FORM>
+__global__ void __launch_bounds__(64 * (C::NW + (FORM != Few::plain ? C::TW : 0))) layer_few_kernel(LayerArgs p) {
+    constexpr bool TERM = FORM != Few::plain;
     constexpr int NI = C::NI, NW = C::NW, WAVES = NW + (TERM ? C::TW : 0);
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = l & 15, q = l >> 4;
@@ -179,7 +241,9 @@ __global__ void __launch_bounds__(64 * (C::NW + (TERM ? C::TW : 0))) layer_few_k
     f32x4 acc[1][NI];
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) acc[0][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (TERM && w >= NW) {
+    if (FORM == Few::own && w >= NW) {
+        own_term<C>(p, rt, c0, w - NW, acc);
+    } else if (TERM && w >= NW) {
         using T = typename C::Term;
         RequestTerm<T> term(p.t, rt, c0, 0, 0, ((RequestList<T>*)(smem + C::BODY))[w - NW], w - NW);
         term.form(acc);
@@ -424,10 +488,12 @@ static hipError_t launch_layer(const LayerArgs& a, int tile_rows, int tile_colum
     });
 }
 
-template <class C>
+template <class C, bool OWN>
 static hipError_t launch_few(const LayerArgs& a, hipStream_t st) {
-    if (a.t.P > 0) return launch_layer<layer_few_kernel<C, true>>(a, 16, C::TN, 64 * (C::NW + C::TW), C::LDS, st);
-    return launch_layer<layer_few_kernel<C, false>>(a, 16, C::TN, 64 * C::NW, C::LDS, st);
+    if constexpr (OWN)
+        if (a.S) return launch_layer<layer_few_kernel<C, Few::own>>(a, 16, C::TN, 64 * (C::NW + C::TW), C::LDS, st);
+    if (a.t.P > 0) return launch_layer<layer_few_kernel<C, Few::term>>(a, 16, C::TN, 64 * (C::NW + C::TW), C::LDS, st);
+    return launch_layer<layer_few_kernel<C, Few::plain>>(a, 16, C::TN, 64 * C::NW, C::LDS, st);
 }
 template <class C>
 static hipError_t launch_ring(const LayerArgs& a, hipStream_t st) {
@@ -456,7 +522,14 @@ static int choose_kind(int M, int K, int N) {
 }
 
 hipError_t launch_quantised_requests(const QuantisedRequestArgs& a, hipStream_t st) {
-    const hipError_t e = a.r.P > 0 ? launch_request_down(a.r, st) : hipSuccess;
+    const int kind = choose_kind(a.r.M, a.r.K, a.r.N);
+    // S formed by every workgroup for itself (own_term), where its rows' columns are few and short enough.  us in a captured graph (with the call from Python), two
+    // launches / one: one row of r = 16, 1024 -> 1024 5.7 / 3.9 (9.6 / 7.3), 4096 -> 4096 7.5 / 6.8 (9.7 / 7.3), 8192 -> 2048 9.8 / 10.1; of 32, 1024 -> 1024 5.8 / 4.7,
+    // 2048 -> 4096 6.5 / 7.1; of 64, 256 -> 256 5.8 / 5.6, 1024 -> 1024 6.1 / 6.3; two of 16, 1024 -> 1024 6.0 / 5.0, 2048 -> 4096 6.5 / 7.3.  (With wider tiles, N = 14336, it was
+    // never faster: 12.2 / 18.2 for one row of 4096.)
+    const int64_t columns = (int64_t)a.r.M * a.r.r;
+    const bool own = a.r.P > 0 && kind == 0 && a.r.M <= 4 && columns * columns * a.r.K <= 1 << 20;
+    const hipError_t e = a.r.P > 0 && !own ? launch_request_down(a.r, st) : hipSuccess;
     if (e != hipSuccess) return e;
     LayerArgs g{};
     g.t.tok = a.r.X;
@@ -472,11 +545,15 @@ hipError_t launch_quantised_requests(const QuantisedRequestArgs& a, hipStream_t 
     g.t.P = a.r.P;
     g.codes = a.codes;
     g.exps = a.exps;
-    int kind = choose_kind(a.r.M, a.r.K, a.r.N);
+    if (own) {
+        g.A = a.r.A;
+        g.s = a.r.s;
+        g.S = a.r.S;
+    }
     switch (kind) {
-        case 0: return a.r.M <= 4 ? launch_few<FewLayer<1, 1, 8, 4, 4>>(g, st) : launch_few<FewLayer<4, 1, 8, 4, 3>>(g, st);
-        case 1: return launch_few<FewLayer<4, 2, 8, 4, 2>>(g, st);
-        case 2: return launch_few<FewLayer<4, 4, 8, 4, 2>>(g, st);
+        case 0: return a.r.M <= 4 ? launch_few<FewLayer<1, 1, 8, 4, 4>, true>(g, st) : launch_few<FewLayer<4, 1, 8, 4, 3>, false>(g, st);
+        case 1: return launch_few<FewLayer<4, 2, 8, 4, 2>, false>(g, st);
+        case 2: return launch_few<FewLayer<4, 4, 8, 4, 2>, false>(g, st);
         case 3: return launch_ring<RingLayer<1, 2, 2, 2, 6, 1>>(g, st);
         case 4: return launch_ring<RingLayer<2, 2, 2, 2, 7, 2>>(g, st);
         case 5: return launch_ring<RingLayer<4, 2, 1, 4, 6, 2>>(g, st);

@@ -183,3 +183,30 @@ def test_most_rows():
     within(Y[:300], ref[:300], bound[:300], "first rows")
     within(Y[-300:], ref[300:], bound[300:], "last rows")
     assert int((Y[300:-300] != 0).sum()) == 0
+
+
+@pytest.mark.parametrize("M,K,N,r,ids,mixed", [
+    (1, 64, 64, 16, "any", False), (1, 4096, 192, 16, "any", True), (1, 1024, 4096, 32, "any", True), (1, 192, 128, 64, "any", True), (1, 256, 64, 64, "each", False),
+    (2, 1024, 320, 16, "each", True), (2, 64, 64, 64, "each", True), (3, 320, 256, 16, "any", True), (4, 256, 128, 16, "each", True), (4, 64, 64, 32, "none", False),
+    (1, 4160, 192, 16, "any", True), (4, 320, 64, 16, "each", False)])                     # (the last two: S from a launch of its own)
+def test_a_few_rows_in_one_launch(M, K, N, r, ids, mixed):
+    """S formed beside the base product: every row with an adapter of its own rank, S as it is returned too, what is past a rank anything."""
+    for seed in range(4):
+        X, codes, exps, A, B, i, s, ranks = _case(M, K, N, r, 5, ids, mixed, seed)
+        if seed and ids != "none":
+            i = (torch.arange(M) + seed).to(torch.int32) % 5
+        if mixed:
+            ranks = torch.tensor([0, 1, r - 1, r // 2, r], dtype=torch.int32)[torch.randperm(5, generator=gen(seed))]
+            for g in range(5):
+                A[g, int(ranks[g]):], B[g, :, int(ranks[g]):] = float("nan"), float("inf")
+        _check((X, codes, exps, A, B, i, s, ranks), ("one launch", M, K, N, r, seed))
+
+
+def test_an_adapter_that_diverged_in_one_launch():
+    X, codes, exps, A, B, ids, s, _ = _case(3, 128, 192, 16, 3, "any", False, 9)
+    ids[:] = torch.tensor([0, 1, -1])
+    want = _check((X, codes, exps, A, B, ids, s, None), "diverged").cpu()
+    B[1, 7, 3], A[2, 5, 5], B[2] = float("inf"), float("nan"), float("nan")
+    Y, _ = binding.lora_requests_quantised_fwd(*(t.cuda() for t in (X, codes, exps, A, B, ids, s)))
+    bad = ~torch.isfinite(Y.cpu())
+    assert bool(bad[1, 7]) and int(bad.sum()) == 1 and torch.equal(Y.cpu()[~bad], want[~bad])
