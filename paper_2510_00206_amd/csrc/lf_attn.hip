@@ -1005,19 +1005,20 @@ static int64_t keys_of_tile(int rows, int group, int64_t max_kv, int window) {
     return window ? std::min<int64_t>(max_kv, (int64_t)window + (rows + group - 1) / group + 16) : max_kv;
 }
 // Parts of a range (plan_attn): as many as make per_unit workgroups to a compute unit, of `least` keys and more, at most `most`; `one`: for one sequence (many
-// rows: for a batch too), otherwise for a batch.
-struct PartsRule { bool few, one; int per_unit, least, most; };
-constexpr PartsRule kParts[] = {{true, true, 2, 512, 1 << 30}, {true, false, 4, 512, 1 << 30}, {true, false, 8, 2048, 1 << 30},
-                                {false, true, 1, 256, 1 << 30}, {false, true, 2, 1024, 1 << 30}, {false, false, 8, 1536, 16}};
+// rows: for a batch too), otherwise for a batch; `four`: over a 4-bit cache alone, whose parts of few keys are read the sooner.
+struct PartsRule { bool few, one; int per_unit, least, most; bool four; };
+constexpr PartsRule kParts[] = {{true, true, 2, 512, 1 << 30, false}, {true, false, 4, 512, 1 << 30, false}, {true, false, 8, 2048, 1 << 30, false},
+                                {true, true, 1, 256, 1 << 30, true}, {true, false, 4, 256, 1 << 30, true},
+                                {false, true, 1, 256, 1 << 30, false}, {false, true, 2, 1024, 1 << 30, false}, {false, false, 8, 1536, 16, false}};
 
 // Rows of partial results (parts x T x H) that no step of at most these sizes exceeds, though a smaller one is cut into more parts.  Of T <= B * max_new tokens in
 // `tiles` of so many rows a sequence, c workgroups to a compute unit make c * kComputeUnits / (tiles * B * G) parts or fewer: parts x T x H is at most c * kComputeUnits
 // rows times those of a sequence (few rows) or of a tile (many), and at most T x H times the parts that one sequence and one tile have.
-int64_t attn_part_rows(int64_t T, int B, int G, int group, int max_new, int64_t max_kv, int window) {
+int64_t attn_part_rows(int64_t T, int B, int G, int group, int max_new, int64_t max_kv, int window, int form) {
     int64_t rows = 0;
     for (const PartsRule& u : kParts) {
         if (u.few ? group > 32 : (int64_t)max_new * group <= 32) continue;
-        if (B == 1 && !u.one) continue;
+        if ((B == 1 && !u.one) || (u.four && form != kCacheFp4)) continue;
         const int64_t units = (int64_t)u.per_unit * kComputeUnits;
         const int64_t of_seq = u.few ? std::min<int64_t>((int64_t)max_new * group, 32) / group * group : 128;
         const int64_t parts = std::min<int64_t>({units / G, keys_of_tile(u.few ? 32 : 128, group, max_kv, window) / u.least, u.most});
@@ -1026,7 +1027,7 @@ int64_t attn_part_rows(int64_t T, int B, int G, int group, int max_new, int64_t 
     return rows;
 }
 
-AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, int window) {
+AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, int window, int form) {
     AttnPlan pl;
     const int64_t rows = (int64_t)max_new * group;
     pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
@@ -1038,12 +1039,15 @@ AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, 
     // keys 236 / 253 (4 to a compute unit), eight of 3000 - 65536 210 / 235 (4), 32 of 200 - 4000 36.9 / 37.8 (8, of 512), 128 of 500 - 3000 173 / 179 (8, of 512), one
     // of 131072 56 / 62 (4); many rows, two of 5003 and 16000, 1021 new 283 / 319 (4), four of 600 - 6000, 300 new 116 / 132 (of 4096), eight of 1000 - 2048, 512
     // new 144 / 207 (of 1024), 16 of 100 - 1000, 64 new 39 / 43 (2, of 512), one of 8192, 1024 new 148 / 154 (4, of 2048), two of 2000 - 3000, 60 new, D = 64
-    // 18 / 19 (of 512), four of 12000 - 61000, 47 new 172 / 178 (39 parts).
+    // 18 / 19 (of 512), four of 12000 - 61000, 47 new 172 / 178 (39 parts).  Over 4 bits, few rows: one sequence 1 of 256 too, a batch 4 of 256: eight sequences of
+    // 100 - 2000 keys 11.1 / 12.6 (4, of 512), four 8.9 / 10.3, one of 4000 10.1 / 11.3, one of 20000 13.4 / 14.1 (2, of 256), longer ones the
+    // same; from four such parts on, since fewer are not worth the join: one of 600 9.0 / 8.5 in one part.
     const int64_t have = std::max<int64_t>(tiles * B * G, 1);
     const auto up_to = [&](int per_unit, int64_t least) { return std::min<int64_t>(per_unit * kComputeUnits / have, keys / least); };
     int64_t parts = 1;
     for (const PartsRule& u : kParts)
-        if (u.few == (pl.rows < 128) && (u.one ? B == 1 || !u.few : B > 1)) parts = std::max(parts, std::min<int64_t>(up_to(u.per_unit, u.least), u.most));
+        if (u.few == (pl.rows < 128) && (!u.four || (form == kCacheFp4 && keys >= 4 * u.least)) && (u.one ? B == 1 || !u.few : B > 1))
+            parts = std::max(parts, std::min<int64_t>(up_to(u.per_unit, u.least), u.most));
     const int64_t step = 128;
     pl.split_keys = (int)(((keys + parts - 1) / parts + step - 1) / step * step);
     if (pl.split_keys < step) pl.split_keys = step;

@@ -82,8 +82,8 @@ hipError_t launch_weights_write(const WeightsArgs& a, hipStream_t st);
 hipError_t launch_weights_read(const WeightsArgs& a, hipStream_t st);
 hipError_t launch_cache_write(const CacheCopyArgs& a, hipStream_t st);
 hipError_t launch_cache_read(const CacheCopyArgs& a, hipStream_t st);
-AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, int window);
-int64_t attn_part_rows(int64_t T, int B, int G, int group, int max_new, int64_t max_kv, int window);      // of any step of at most these sizes
+AttnPlan plan_attn(int B, int G, int group, int D, int max_new, int64_t max_kv, int window, int form);
+int64_t attn_part_rows(int64_t T, int B, int G, int group, int max_new, int64_t max_kv, int window, int form);      // of any step of at most these sizes
 hipError_t launch_attn(AttnArgs a, const AttnPlan& p, int max_new, hipStream_t st);
 hipError_t launch_request_down(const RequestArgs& a, hipStream_t st);       // S alone
 hipError_t launch_requests(const RequestArgs& a, hipStream_t st);

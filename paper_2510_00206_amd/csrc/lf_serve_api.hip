@@ -226,8 +226,8 @@ size_t lora_paged_attn_workspace_bytes(const lora_kv_cache* cache, int64_t T, in
     if (T == 0 || B == 0 || max_new == 0) return 256;
     const int group = H / c.heads;
     // (its own plan too: more tokens than sequences of max_new can have are allowed)
-    return std::max({(size_t)256, attn_scratch(plan_attn((int)B, c.heads, group, c.D, (int)max_new, max_kv, window), T, H, c.D),
-                     attn_scratch((size_t)attn_part_rows(T, (int)B, c.heads, group, (int)max_new, max_kv, window), c.D)});
+    return std::max({(size_t)256, attn_scratch(plan_attn((int)B, c.heads, group, c.D, (int)max_new, max_kv, window, c.form), T, H, c.D),
+                     attn_scratch((size_t)attn_part_rows(T, (int)B, c.heads, group, (int)max_new, max_kv, window, c.form), c.D)});
 }
 
 lora_status lora_paged_attn_fwd(const lora_bf16* q, const lora_kv_cache* cache, const int32_t* table, const int32_t* offsets, const int32_t* kv_lens,
@@ -246,7 +246,7 @@ lora_status lora_paged_attn_fwd(const lora_bf16* q, const lora_kv_cache* cache, 
     if (misaligned(q) || misaligned(out) || misaligned(workspace, 256) || misaligned(table, 4) || misaligned(offsets, 4) || misaligned(kv_lens, 4))
         return LORA_ERR_ALIGN;
     if (max_pages >= 1ll << (30 - a.c.page_shift)) return LORA_ERR_UNSUPPORTED;
-    const AttnPlan pl = plan_attn((int)B, a.c.heads, H / a.c.heads, a.c.D, (int)max_new, max_kv, window);
+    const AttnPlan pl = plan_attn((int)B, a.c.heads, H / a.c.heads, a.c.D, (int)max_new, max_kv, window, a.c.form);
     if ((max_new * (H / a.c.heads) / pl.rows + 1) * pl.splits * B * a.c.heads >= 1ll << 24) return LORA_ERR_UNSUPPORTED;     // (threads of a launch)
     if (workspace_bytes < attn_scratch(pl, T, H, a.c.D)) return LORA_ERR_WORKSPACE;
     a.q = q;

@@ -1,6 +1,8 @@
 """The entry points around 4-bit weights and caches refuse bad arguments on the host, before anything is enqueued, with the documented status."""
 import ctypes as C
+import math
 import os
+import random
 
 import pytest
 
@@ -94,3 +96,18 @@ def test_cache_in_4_bits(lib):
     for dim in (64, 128):
         one, other = (lib.lora_paged_attn_workspace_bytes(_cache(dim=dim, heads=8, fp8=form), 4, 32, 4, 1, 131072, 0) for form in (1, FP4))
         assert one == other > 256
+
+
+def test_workspace_of_smaller_steps(lib):
+    """What the query returns for a step is enough for every smaller one, which may be cut into more parts."""
+    rng = random.Random(3)
+    log = lambda lo, hi: int(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.9))))
+    for _ in range(4000):
+        G, group = rng.choice((1, 2, 4, 8)), rng.choice((1, 2, 4, 5, 8, 33, 40))
+        cache = _cache(heads=G, dim=rng.choice((64, 128)))
+        B, new, kv, window = log(1, 200), rng.choice((1, log(1, 600))), log(1, 200000), rng.choice((0, 0, log(1, 5000)))
+        T = log(1, B * new)
+        B2, new2, kv2 = log(1, B), log(1, new), log(1, kv)
+        T2 = log(1, min(T, B2 * new2))
+        big, small = (lib.lora_paged_attn_workspace_bytes(cache, t, G * group, b, n, k, window) for t, b, n, k in ((T, B, new, kv), (T2, B2, new2, kv2)))
+        assert 256 <= small <= big, (G, group, (T, B, new, kv), (T2, B2, new2, kv2), window)
