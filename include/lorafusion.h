@@ -292,7 +292,7 @@ lora_status lora_ceiling_hbm_read(const void* src, size_t bytes, uint32_t* sink,
  * their new tokens over a cache of keys and values.  The same conventions as above; "device arrays" are read by the kernels, so their
  * values are not checked on the host, and what is out of range in them is handled as each call says.  Strides (ld*) are the
  * distances of rows in elements, multiples of 8, the heads of a row lying side by side.  Sums, norms and the softmax are fp32 and outputs are
- * rounded once; what stands between two products is rounded to bf16 before the second: S of lora_requests_fwd and the weights of
+ * rounded once; what stands between two products is rounded to bf16 before the second: S of lora_requests_fwd (and _quantised_fwd) and the weights of
  * lora_paged_attn_fwd. */
 
 /* Forward of a batch in which every row names its adapter:
@@ -372,7 +372,7 @@ lora_status lora_kv_cache_read(const lora_kv_cache* cache, const int64_t* slots,
 
 /* lora_qk_norm_rope_fwd and lora_kv_cache_write in one pass: the normalised and turned queries go to q_out [M,H,dim], the keys and v [M,heads,dim] to their slots.
  * gamma_q and gamma_k NULL (both): no norm, the rotation alone; eps is checked all the same.  Keys that the cache holds in fewer bits are formed in 64 bits and rounded
- * once, to its codes (magnitudes from 2^128 on count as not finite); everything else is as in those two calls, a row outside the tables: zeros for query
+ * once, to its codes (what is past the range of fp32 counts as not finite); everything else is as in those two calls, a row outside the tables: zeros for query
  * and keys, a slot outside the cache: left out.  q_out may be q.  dim, rot, H and M as in the first. */
 lora_status lora_kv_cache_append(const lora_kv_cache* cache, const lora_bf16* q, const lora_bf16* k, const lora_bf16* v, const lora_bf16* gamma_q,
                                  const lora_bf16* gamma_k, const float* cos_table, const float* sin_table, const int32_t* pos, const int64_t* slots, int64_t M,

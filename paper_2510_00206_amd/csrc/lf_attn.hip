@@ -334,7 +334,8 @@ __device__ __forceinline__ void have(bf16x8 (&f)[N]) {
 // NQ blocks of 16 rows; a wave takes every fourth tile of 32 keys, and asks for the next tile's values before and its keys behind the scores of this
 // one.  Measured (a read of 2 GiB: 6.0 TB/s): four sequences of 33000 - 131072 keys, bf16, 1.34 GB, 229 us, 5.9 TB/s; 32 of 200 - 4000, fp8, 139 MB, 32 us, 4.3 TB/s,
 // some 6 us of it until the first keys are there (lengths, page numbers, keys: one after the other).  Two tiles of fp8 under way, with the registers that
-// takes, 41 us for the latter launch and the join instead of 37.
+// takes, 41 us for the latter launch and the join instead of 37.  4 bits: the former 71 us (356 MB, 5.0 TB/s), the latter 19 (74 MB, 3.8 TB/s), and 21.7 with the join.  For
+// 4 bits and one block of rows D = 128 takes 148 registers, three waves to a SIMD; held to 128, for four, it spills and takes twice as long.
 template <int D, int FORM, int NQ>
 struct Few {
     static constexpr int KEYS = 32, WAVES = 4;
@@ -569,7 +570,9 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
 // tile n + 1, the softmax of tile n and the values of tile n - 1 are one stream of instructions, in which the vector ones stand between the matrix
 // ones, two to each: only those of the same wave run beside a matrix instruction, those of other waves wait for it.  Measured: two
 // prompts' 1021 new tokens over 5003 and 16000 keys, 32 heads of 128 to 8, 250 GFLOP, 265 us, 940 TFLOP/s (a product of 8192^3: 1320); bound by the issue of
-// instructions (a step of 64 keys takes 3300 cycles, of which its 64 matrix instructions and the 64 of the SIMD's other wave 2050).
+// instructions (a step of 64 keys takes 3300 cycles, of which its 64 matrix instructions and the 64 of the SIMD's other wave 2050).  With the join 280; over 4 bits 330:
+// two waits and two widenings a step.  Codes into registers instead of LDS, widened in one go 345, between the matrix instructions 361 (the registers are
+// all taken); through two places in LDS, between the matrix instructions, 359.
 template <int D, int FORM>
 struct Many {
     static constexpr int KEYS = 64, ROWS = 128, NQ = 2;

@@ -104,9 +104,11 @@ __device__ __forceinline__ int exp_byte(bool split, int r, int c, int q) { retur
 __device__ __forceinline__ int half_exp_byte(int r, int c, int q) { return 4 * r + 2 * (c & 1) + (q >> 1); }
 
 // ---- few rows ---------------------------------------------------------------------------------------
-// Bound by the reading of the weights.  A workgroup has up to 16 rows (of which it brings 4 XC) and NI x 16 columns, its NW waves every NW-th block of the contraction, which each brings into a ring of
+// Bound by the reading of the weights, of which a launch of a few us sees mostly the latency.  A workgroup has up to 16 rows (of which it brings 4 XC) and NI x 16 columns, its NW waves every NW-th block of the contraction, which each brings into a ring of
 // its own of D blocks, with no barrier; the adapters' term is formed by TW waves of its own beside them, which share its steps.  Sums of the waves are added in LDS
-// in a fixed order.
+// in a fixed order.  Measured (us, in a captured graph, the first product's launch included where there are adapters): one row 4096 -> 14336, r = 16, 12.2 (31 MB of weights; codes
+// from memory straight into the lanes that use them 22); 16 rows 4096 -> 6144, no adapters 6.2, 12 of r = 16 10.1; 16 rows 14336 -> 4096 11.8 and 17.2.  Three blocks
+// to a ring of the 16 x 32 tiles instead of two, which is all that LDS holds: the same.
 template <int XC_, int NI_, int NW_, int TW_, int D_>
 struct FewLayer {
     static constexpr int XC = XC_, NI = NI_, NW = NW_, TW = TW_, D = D_, TN = 16 * NI;
@@ -268,7 +270,10 @@ __global__ void __launch_bounds__(64 * (C::NW + (FORM != Few::plain ? C::TW : 0)
 // X, the codes and the exponents go through a ring of NS blocks in LDS, filled by CW waves that do nothing else.  A wave's 16 MI x 16 NI tile is one stream of
 // instructions over the blocks: a matrix instruction to a slot, and between them the reads of the fragments of X, three ahead of their use, and the widening of the next
 // step's codes.  (Codes straight from memory into the registers of the lanes that use them, 16 bytes of a row to each: neighbouring lanes have other rows, so that a
-// load takes 64 cycles of the address unit instead of 16, and one of exponents, a byte to a lane, as many; 2048 rows, 4096 -> 4096: 71 us, 1.9 us a block.)
+// load takes 64 cycles of the address unit instead of 16, and one of exponents, a byte to a lane, as many; 2048 rows, 4096 -> 4096: 71 us, 1.9 us a block; this 50, 1363 TFLOP/s.)  The term comes before the first block, while the ring is
+// filled: 96 rows of 64 adapters, r = 64, 4096 -> 14336: 42 us with it, 18 without.  Formed meanwhile by waves of its own, four or eight, which meet the others at the ring's barriers, with
+// B in registers or through LDS, a row's 64 bytes to four lanes: 40, and 5 - 8 % more than now for adapters of r = 16, K = 1024; it is B's lines that take the
+// time, 95 MB in pieces of 64 bytes.
 template <int MI_, int NI_, int WM_, int WN_, int NS_, int CW_>
 struct RingLayer {
     static constexpr int MI = MI_, NI = NI_, WM = WM_, WN = WN_, NS = NS_, CW = CW_, NW = WM * WN, THREADS = 64 * NW;

@@ -67,13 +67,15 @@ __device__ __forceinline__ void request_row(const RequestDownArgs& p, int row, i
 __global__ void __launch_bounds__(64) request_rows_kernel(RequestDownArgs p) { request_row(p, blockIdx.x, blockIdx.y * kDownColumns); }
 
 // Many rows: the 16-row tiles of one adapter by MFMAs, 16 columns of the rank to a workgroup, every eighth 64-deep slab of the contraction to a
-// wave, four of them under way at once (a lane's two 16-byte loads of a row's slab lie side by side).  The rows of the other tiles go to
+// wave, four of them under way at once.  A load brings whole 128-byte pieces of eight rows, eight lanes to a piece, which go through 4 KB of LDS of the wave's own into the
+// fragments' layout: loads in that layout, 16 bytes to a lane and neighbouring lanes in other rows, take four times as long in the address unit (whole layer, 4096 -> 1024, so / this:
+// 2048 rows, three chunks and 37 single ones, r = 32 37 / 34 us; 8000 rows in two chunks, r = 64 130 / 109).  The rows of the other tiles go to
 // further workgroups of the launch, a wave for each row and two columns, which find nothing to do where the tile is of one adapter.
 // (One after the other in their own workgroups the adapters of such tiles, 37 requests of one token among 2048 rows, took 57 us.)
-constexpr int kTileWaves = 8;
+constexpr int kTileWaves = 8, kSlabPart = 16 * 128;        // 16 rows of a slab of X, or of A
 struct RequestTileArgs { RequestDownArgs d; int tiles, parts; };       // parts: of the rank, 16 columns each
 __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestTileArgs a) {
-    __shared__ f32x4 red[kTileWaves][64];
+    __shared__ __attribute__((aligned(16))) char stage[kTileWaves][2 * kSlabPart];
     const RequestDownArgs& p = a.d;
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool by_rows = (int)blockIdx.x >= a.tiles * a.parts;
@@ -95,31 +97,48 @@ __global__ void __launch_bounds__(64 * kTileWaves) request_tile_kernel(RequestTi
     const int j0 = (int)blockIdx.x % a.parts * 16, rank = g < 0 ? 0 : p.ranks ? min(p.ranks[g], p.r) : p.r;
     f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
     if (rank > j0) {
-        const lora_bf16* x = p.X + (int64_t)min(row, p.M - 1) * p.K + 16 * (l >> 4);
-        const lora_bf16* ag = p.A + ((int64_t)g * p.r + j0 + (l & 15)) * p.K + 16 * (l >> 4);
+        // of a load: row 8 h + l / 8, chunk l % 8 of its eight; in LDS a chunk of row n lies at its number ^ (n & 7)
+        const lora_bf16 *x[2], *ag[2];
+        uint32_t to[2], from[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int n = 8 * h + l / 8, c = l & 15;
+            x[h] = p.X + (int64_t)min(row0 + n, p.M - 1) * p.K + 8 * (l % 8);
+            ag[h] = p.A + ((int64_t)g * p.r + j0 + n) * p.K + 8 * (l % 8);
+            to[h] = n * 128 + ((l % 8 ^ (n & 7)) << 4);
+            from[h] = c * 128 + (((2 * (l >> 4) + h) ^ (c & 7)) << 4);
+        }
         constexpr int U = 4;
         for (int k = 64 * w; k < p.K; k += 64 * kTileWaves * U) {
-            bf16x8 xf[U][2], af[U][2];
+            u32x4 xr[U][2], ar[U][2];
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int at = min(k + 64 * kTileWaves * u, p.K - 64) + 8 * h;       // (past the end: brought, not used)
-                    xf[u][h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(x + at));
-                    af[u][h] = __builtin_bit_cast(bf16x8, *(const u32x4*)(ag + at));
+                    const int at = min(k + 64 * kTileWaves * u, p.K - 64);       // (past the end: brought, not used)
+                    xr[u][h] = *(const u32x4*)(x[h] + at);
+                    ar[u][h] = *(const u32x4*)(ag[h] + at);
                 }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (k + 64 * kTileWaves * u < p.K)
+            for (int u = 0; u < U; ++u) {
+                if (k + 64 * kTileWaves * u >= p.K) break;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) acc = LF_MFMA(af[u][h], xf[u][h], acc);
+                for (int h = 0; h < 2; ++h) {
+                    *(u32x4*)(stage[w] + to[h]) = xr[u][h];
+                    *(u32x4*)(stage[w] + kSlabPart + to[h]) = ar[u][h];
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    acc = LF_MFMA(__builtin_bit_cast(bf16x8, *(const u32x4*)(stage[w] + kSlabPart + from[h])),
+                                  __builtin_bit_cast(bf16x8, *(const u32x4*)(stage[w] + from[h])), acc);
+            }
         }
     }
-    red[w][l] = acc;
+    *(f32x4*)(stage[w] + 16 * l) = acc;
     __syncthreads();
     if (w || row >= p.M) return;
 #pragma unroll
-    for (int i = 1; i < kTileWaves; ++i) acc += red[i][l];
+    for (int i = 1; i < kTileWaves; ++i) acc += *(const f32x4*)(stage[i] + 16 * l);
     const int c = j0 + 4 * (l >> 4);
     const float s = g < 0 ? 0.f : p.s[g];
     float o[4];

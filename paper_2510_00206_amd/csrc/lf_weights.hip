@@ -1,5 +1,6 @@
 // Weights into 4 bits (e2m1 and a power of two for 32 entries of a row, lf_quant.h) and back to bf16, which holds their values exactly.  Bound by HBM: 2 + 17 / 32
-// bytes an entry.  Rows are whole groups, so that a matrix is one run of entries; eight to a lane.
+// bytes an entry.  Rows are whole groups, so that a matrix is one run of entries; eight to a lane, four times.  Measured: 1024 x 4096 written 4.1 us, read 3.8 (11 MB: launch and
+// one latency); 14336 x 4096 read 27.1 us (149 MB, 5.5 TB/s).
 #include <algorithm>
 
 #include "lf_serve.h"
