@@ -1,5 +1,5 @@
 // The LoRA linear layer for many requests over 4-bit weights:
-//     S[i] = s_g X[i] A_g^T             lf_requests.hip
+//     S[i] = s_g X[i] A_g^T             lf_requests.hip; of a few short rows here (own_term)
 //     Y[i] = X[i] W^T + S[i] B_g^T,     W[n,k] = e2m1(codes[n,k]) 2^(exps[n,k/32] - 127)
 // The codes are widened to bf16 (exact, one instruction for two) on their way into the matrix instructions, so that no product is rounded and the sums
 // are those of bf16 weights.  A lane takes 16 bytes of a row of codes: 32 entries, which share one power of two.  Its 16-byte load is four matrix steps, for
