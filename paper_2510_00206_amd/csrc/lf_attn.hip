@@ -335,7 +335,8 @@ __device__ __forceinline__ void have(bf16x8 (&f)[N]) {
 // one.  Measured (a read of 2 GiB: 6.0 TB/s): four sequences of 33000 - 131072 keys, bf16, 1.34 GB, 229 us, 5.9 TB/s; 32 of 200 - 4000, fp8, 139 MB, 32 us, 4.3 TB/s,
 // some 6 us of it until the first keys are there (lengths, page numbers, keys: one after the other).  Two tiles of fp8 under way, with the registers that
 // takes, 41 us for the latter launch and the join instead of 37.  4 bits: the former 71 us (356 MB, 5.0 TB/s), the latter 19 (74 MB, 3.8 TB/s), and 21.7 with the join.  For
-// 4 bits and one block of rows D = 128 takes 148 registers, three waves to a SIMD; held to 128, for four, it spills and takes twice as long.
+// 4 bits and one block of rows D = 128 takes 148 registers, three waves to a SIMD; held to 128, for four, it spills and takes twice as long; with two
+// tiles under way 177, two waves, 28 us instead of 21.7, and level where there are few parts.
 template <int D, int FORM, int NQ>
 struct Few {
     static constexpr int KEYS = 32, WAVES = 4;
