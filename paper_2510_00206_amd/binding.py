@@ -502,17 +502,20 @@ class KVCache:
     def __init__(self, k, v, k_exp=None, v_exp=None):
         shape = k.shape
         assert len(shape) == 4 and v.shape == shape, "k and v are [pages, heads, page, dim]"
-        self.pages, self.heads, self.page, self.dim = shape
-        form, exps = {_FP8: (1, shape[:3]), _U8: (KV_FP4, (*shape[:3], shape[3] // 16))}.get(k.dtype, (0, None))
-        if form == KV_FP4:
-            self.dim *= 2
+        self.pages, self.heads, self.page, self.dim = pages, heads, page, dim = shape
+        dtype, form, exps = k.dtype, 0, None
+        if dtype is _U8:
+            self.dim = 2 * dim
+            form, exps = KV_FP4, (pages, heads, page, dim // 16)
+        elif dtype is _FP8:
+            form, exps = 1, (pages, heads, page)
         if form:
             assert k_exp is not None and v_exp is not None and k_exp.shape == v_exp.shape == exps, "exponents: one for every token and head, 4 bits for every 32 entries"
             self.tensors = (k, v, k_exp, v_exp)
-            self._c = CacheArrays(_at(k, k.dtype), _at(v, k.dtype), _at(k_exp, _U8), _at(v_exp, _U8), shape[0], shape[2], shape[1], self.dim, form)
+            self._c = CacheArrays(_at(k, dtype), _at(v, dtype), _at(k_exp, _U8), _at(v_exp, _U8), pages, page, heads, self.dim, form)
         else:
             self.tensors = (k, v, None, None)
-            self._c = CacheArrays(_at(k, _BF16), _at(v, _BF16), None, None, shape[0], shape[2], shape[1], shape[3], 0)
+            self._c = CacheArrays(_at(k, _BF16), _at(v, _BF16), None, None, pages, page, heads, dim, 0)
         self._ref = C.byref(self._c)
 
     @classmethod
