@@ -8,7 +8,7 @@ adapter (lora_requests_fwd), queries and keys are normalised and turned (lora_qk
 (lora_kv_cache_write), the new tokens attend over it (lora_paged_attn_fwd), and the output projection takes the adapters again.  Prompts may come
 in chunks, beside requests that decode: what a step needs to know of them are arrays on the GPU, so that a step of fixed size can be
 captured in a HIP graph and replayed.
-Serving over 4 bits: the same block after quantise(): both projections over 4-bit weights (lora_requests_quantised_fwd), queries, keys and values from the
+Serving over 4 bits (and training over the same weights, widened for the step): the same block after quantise(): both projections over 4-bit weights (lora_requests_quantised_fwd), queries, keys and values from the
 projection to attention and the cache in one call (lora_kv_cache_append), which may be a 4-bit cache too.
 Training: the same projection and norm with the backward passes of the library."""
 import torch
@@ -39,7 +39,7 @@ class AttentionBlock:
         self.four_bits = None
 
     def quantise(self):
-        """Serve over 4-bit weights from here on; the bf16 ones stay for training.  -> the block"""
+        """4-bit weights from here on, in serving and (widened for the step) in training, so that adapters meet the weights that they are trained on.  -> the block"""
         self.four_bits = binding.lora_weights_write(self.w_qkv), binding.lora_weights_write(self.w_out)
         return self
 
@@ -73,7 +73,8 @@ class AttentionBlock:
         -> (q, k, v), (dx, dA, dB, dgamma_q, dgamma_k)"""
         H, G, D = self.heads, self.kv_heads, self.dim
         a, b, s = self.a_qkv[adapter].contiguous(), self.b_qkv[adapter].contiguous(), float(self.scale[adapter])
-        qkv, saved = binding.lora_fwd(x, self.w_qkv, a, b, s, dropout, seed)
+        w = binding.lora_weights_read(*self.four_bits[0]) if self.four_bits else self.w_qkv
+        qkv, saved = binding.lora_fwd(x, w, a, b, s, dropout, seed)
         part = lambda t: tuple(t[:, i * D:j * D].unflatten(1, (j - i, D)) for i, j in ((0, H), (H, H + G), (H + G, H + 2 * G)))
         q, k, v = part(qkv)
         turned = binding.lora_qk_norm_rope_fwd(q, k, self.gamma_q, self.gamma_k, self.cos, self.sin, positions)
@@ -81,7 +82,7 @@ class AttentionBlock:
         pq, pk, pv = part(d_qkv)
         _, _, dgq, dgk = binding.lora_qk_norm_rope_bwd(q, k, self.gamma_q, self.gamma_k, self.cos, self.sin, positions, dq, dk, dq=pq, dk=pk)
         pv.copy_(dv)
-        dx, da, db = binding.lora_bwd(x, self.w_qkv, a, b, saved, d_qkv, s, dropout, seed)
+        dx, da, db = binding.lora_bwd(x, w, a, b, saved, d_qkv, s, dropout, seed)
         return (*turned, v), (dx, da, db, dgq, dgk)
 
 

@@ -127,6 +127,40 @@ def test_replays_of_captured_steps(form):
             assert torch.equal(a[p // 16, :, p % 16].view(torch.uint8), b[p // 16, :, p % 16].view(torch.uint8))
 
 
+def test_training_step():
+    """Gradients of the projection over the widened weights, with norm and rotation, against autograd in 64 bits over what the codes hold (no dropout): within what the roundings
+    to bf16 of qkv, its gradient and the saved S leave, four of them (2-norm); and a difference along dA and dB."""
+    block = _block()
+    H, G, D, M = 4, 2, 64, 50
+    g = gen(4)
+    draw = lambda *shape: torch.randn(shape, generator=g).to(BF16)
+    x, dq, dk, dv = draw(M, 320), draw(M, H, D), draw(M, G, D), draw(M, G, D)
+    pos = torch.randint(0, 300, (M,), generator=g, dtype=torch.int32)
+    outs, grads = block.train(x.cuda(), pos.cuda(), dq.cuda(), dk.cuda(), dv.cuda(), adapter=2, dropout=0.0)
+    c = lambda t: t.detach().cpu().to(F64).clone().requires_grad_()
+    W = widened4(*(t.cpu() for t in block.four_bits[0]))
+    leaves = X, A, B, gq, gk = c(x), c(block.a_qkv[2]), c(block.b_qkv[2]), c(block.gamma_q), c(block.gamma_k)
+
+    def forward(X, A, B, gq, gk):
+        qkv = X @ W.t() + 2.0 * ((X @ A.t()) @ B.t())
+        q, k, v = (qkv[:, i * D:j * D].unflatten(1, (j - i, D)) for i, j in ((0, H), (H, H + G), (H + G, H + 2 * G)))
+        return *(norm_rope(t, gm, block.cos.cpu(), block.sin.cpu(), pos, 1e-6, False)[0] for t, gm in ((q, gq), (k, gk))), v
+    ys = forward(*leaves)
+    for got, ref in zip(outs, ys):
+        assert float(((got.cpu().to(F64) - ref).norm() / ref.norm()).detach()) <= 4 * 2.0 ** -8
+    weights = [t.to(F64) for t in (dq, dk, dv)]
+    refs = torch.autograd.grad(ys, leaves, weights)
+    for got, ref, name in zip(grads, refs, ("dx", "dA", "dB", "dgamma_q", "dgamma_k")):
+        assert float((got.cpu().to(F64) - ref).norm() / ref.norm()) <= 4 * 2.0 ** -8, name
+    loss = lambda A, B: sum((y * w).sum() for y, w in zip(forward(X, A, B, gq, gk), weights))
+    with torch.no_grad():
+        for i, got in ((1, grads[1].cpu().to(F64)), (2, grads[2].cpu().to(F64))):
+            h = 1e-4 / float(got.norm())
+            ends = [loss(*(t + (sign * h * got if j == i else 0) for j, t in ((1, A), (2, B)))) for sign in (1, -1)]
+            slope = float(ends[0] - ends[1]) / (2 * h)
+            assert abs(slope - float((refs[i] * got).sum())) <= 1e-4 * abs(slope) and abs(slope - float((got * got).sum())) <= 8 * 2.0 ** -8 * abs(slope)
+
+
 def test_a_busy_stream():
     """All calls of a step wait for the work that its stream still has before them: launched anywhere else they would read zeros."""
     block = _block()
