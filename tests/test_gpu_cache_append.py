@@ -185,3 +185,29 @@ def test_write_and_read_in_4_bits(M, G, D, page):
             ref[2:4] = 0
         got, nan = back[i].cpu().to(F64), torch.isnan(ref)
         assert torch.equal(torch.isnan(got), nan) and torch.equal(got[~nan], ref[~nan])
+
+
+@pytest.mark.parametrize("form", ["bf16", "fp4"])
+def test_a_launch_and_another(form):
+    """More rows than a launch has (2^24 of one query head and one of keys and values): the first ones, those on either side of 2^24 and the last ones; the others of zeros."""
+    M, D, page = (1 << 24) + 37, 32, 1024
+    g = gen(12)
+    rows = torch.cat([torch.arange(20), torch.arange((1 << 24) - 20, M)])
+    qkv = torch.zeros((M, 3 * D), dtype=BF16, device="cuda")
+    some = normal(g, (rows.numel(), 3 * D))
+    qkv[rows.cuda()] = some.cuda()
+    pos = torch.zeros((M,), dtype=torch.int32, device="cuda")
+    slots = torch.arange(M, device="cuda").flip(0)
+    ang = torch.rand((1, D // 2), generator=g, dtype=F64) * 6.3
+    cos, sin = ang.cos().to(F32), ang.sin().to(F32)
+    gq, gk = (normal(g, (D,), 0.3, 1.0) for _ in range(2))
+    cache = binding.KVCache.empty(M // page + 1, page, 1, D, fp4=form == "fp4")
+    q, k, v = (qkv[:, i * D:(i + 1) * D].unflatten(1, (1, D)) for i in range(3))
+    out = binding.lora_kv_cache_append(cache, q, k, v, cos.cuda(), sin.cuda(), pos, slots, gq=gq.cuda(), gk=gk.cuda(), eps=EPS)
+    sq, sk, sv = (some[:, i * D:(i + 1) * D].unflatten(1, (1, D)) for i in range(3))
+    at = torch.zeros(rows.numel(), dtype=torch.int32)
+    ref, bound = _ref(sq, gq, cos, sin, at, False)
+    within(out[rows.cuda()], ref, bound, "queries")
+    kref, kbound = _ref(sk, gk, cos, sin, at, False)
+    _compare(form, cache, slots[rows.cuda()].cpu(), kref, kbound, sv, form)
+    assert int((out[20:(1 << 24) - 20] != 0).sum()) == 0            # (zeros of either sign: 0 x a negative cosine)
