@@ -651,7 +651,11 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
         return (uint32_t)((row * 2 * D + le % (D / 8) * 16) ^ ((keys ? k_off<D>(row, 0) : v_off<D>(row, 0)) & (2 * D - 1)));
     };
     constexpr int RPR = 1024 / H::BYTES < 16 ? 1024 / H::BYTES : 16, NR = 16 / RPR;     // fp8, 4 bits: rows of a copy, copies of a block
-    constexpr int RAW_LANES = RPR * H::CHUNKS;              // ... lanes that have something of it (the others bring the same again)
+    constexpr uint32_t RAW_LANES = RPR * H::CHUNKS;         // ... lanes that have something of it (the others bring the same again)
+    static_assert(RAW_LANES == 64 || RAW_LANES == 32, "a power of two");
+    static_assert(!RAW || H::EXPS == 1 || H::EXPS == H::CHUNKS, "an exponent to a head, or to a lane's chunk");
+    // (unsigned, and masked only where there are fewer than 64: the loop is bound by the issue of instructions, and the compiler doesn't know a lane's range)
+    auto raw_lane = [&] { return RAW_LANES < 64 ? (uint32_t)lane_here() & (RAW_LANES - 1) : (uint32_t)lane_here(); };
     uint8_t ex[NR];                                         // ... and of this lane's chunk of each the exponent
     // first head entry of the wave's block in the tiles whose values (at_v) and keys (at_k) are asked for next, and in the one between; page of the
     // one after
@@ -664,11 +668,10 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
     auto bring = [&](bool keys, int64_t at, int stage) {
         const char* from = source(keys, at);
         if constexpr (RAW) {
-            const int le = lane_here() % RAW_LANES;
+            const uint32_t le = raw_lane();
             copy_raw<NR>(from, le * 16, __builtin_amdgcn_readfirstlane(lds + C::RAW + w * C::WAVE_RAW));
 #pragma unroll
-            for (int i = 0; i < NR; ++i)
-                ex[i] = (keys ? p.c.k_exp : p.c.v_exp)[(at + i * RPR + le / H::CHUNKS) * H::EXPS + le % H::CHUNKS * H::EXPS / H::CHUNKS];
+            for (int i = 0; i < NR; ++i) ex[i] = (keys ? p.c.k_exp : p.c.v_exp)[(at + i * RPR) * H::EXPS + (H::EXPS == 1 ? le / H::CHUNKS : le)];
         } else {
             const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds + (keys ? 0 : 2 * C::TILE) + stage * C::TILE + w * 32 * D + D / 64 * 1024);
             if (keys) copy_block<D, true>(from, lane_source(true), m0);
@@ -678,9 +681,9 @@ __global__ void __launch_bounds__(256, 2) attn_many_kernel(AttnArgs p) {
     // fp8, 4 bits: row and first chunk in the tile of 16 bytes of copy i, and what they are widened to
     struct Wide { int row, chunk; u32x4 v[H::WIDE]; };
     auto widened = [&](int i) {
-        const int le = lane_here() % RAW_LANES;
+        const uint32_t le = raw_lane();
         const u32x4 raw = *(const u32x4*)(smem + C::RAW + w * C::WAVE_RAW + i * 1024 + le * 16);
-        Wide x{16 * w + i * RPR + le / H::CHUNKS, le % H::CHUNKS * H::WIDE, {}};
+        Wide x{16 * w + i * RPR + (int)(le / H::CHUNKS), (int)(le % H::CHUNKS) * H::WIDE, {}};
         if constexpr (FORM == kCacheFp4) {
             const float sc = exp2_of_biased(ex[i]);
 #pragma unroll
