@@ -2,15 +2,17 @@
 // e2m1 values and one power of two for 32 entries (lf_quant.h): a value is rounded once, to three fraction bits or one, and what is read back
 // (value x scale) is exact in bf16.  Bound by HBM: 3 + 1 / D bytes an element (bf16: 4; 4 bits: 2 + 17 / 32).  Eight entries to a lane, a head to 8, 16
 // or 32 lanes.
-// Measured: 2085 tokens of 8 heads of 128 to fp8, 13 MB, 5.5 us (slot, then the head: two latencies), 32768 tokens, 203 MB, 56 us; 29999 tokens read back from
-// fp8, 185 MB, 44 us; with two or four heads to a lane, all their loads under way, 48; 2085 tokens of 8 heads of 128 read back from 4 bits 4.8 us.
+// Measured in a captured graph, us: tokens of 8 heads of 128 to fp8, 2085 (13 MB) 4.75 (slot, then the head: two latencies), 32768 (203 MB) 50.9, to bf16 4.6 and 53.6; 29999
+// tokens read back from fp8, 185 MB, 44; with two or four heads to a lane, all their loads under way, 48.
 #include "lf_quant.h"
 #include "lf_serve.h"
 
 namespace lf {
 
-template <int GL>
+// A kernel for each form: 8 waves to a SIMD and some 250 instructions each are most of what 2085 tokens take, so that what is not of the form counts.
+template <int GL, int FORM>
 __global__ void __launch_bounds__(256) cache_write_kernel(CacheCopyArgs p) {
+    p.c.form = FORM;
     const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / GL;       // token, head
     const int j = threadIdx.x % GL;
     const bool keys = blockIdx.y == 0;
@@ -73,7 +75,10 @@ static hipError_t with_lanes(const CacheCopyArgs& a, F&& f) {
 hipError_t launch_cache_write(const CacheCopyArgs& a, hipStream_t st) {
     return with_lanes(a, [&](auto gl) {
         const int64_t blocks = (a.M * a.c.heads * gl() + 255) / 256;
-        hipLaunchKernelGGL(cache_write_kernel<gl()>, dim3((unsigned)blocks, 2), dim3(256), 0, st, a);
+        const auto launch = [&](auto form) { hipLaunchKernelGGL((cache_write_kernel<gl(), form()>), dim3((unsigned)blocks, 2), dim3(256), 0, st, a); };
+        if (a.c.form == kCacheFp4) launch(std::integral_constant<int, kCacheFp4>{});
+        else if (a.c.form == kCacheFp8) launch(std::integral_constant<int, kCacheFp8>{});
+        else launch(std::integral_constant<int, kCacheBf16>{});
         return hipGetLastError();
     });
 }

@@ -29,9 +29,16 @@ template <int LANES>
 __device__ __forceinline__ u32x2 to_fp8(const float (&x)[8], uint32_t& exponent) {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t b = __builtin_bit_cast(uint32_t, x[i]) & 0x7FFFFFFFu;
-        top = max(top, b < 0x7F800000u ? b : 0u);
+    for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, x[i]) & 0x7FFFFFFFu);
+    // (of the wave; without such values they are not looked for entry by entry: 2085 tokens of 8 heads of 128 to the cache 4.75 us, always 5.3)
+    const bool odd = __any(top >= 0x7F800000u);
+    if (odd) {
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t b = __builtin_bit_cast(uint32_t, x[i]) & 0x7FFFFFFFu;
+            top = max(top, b < 0x7F800000u ? b : 0u);
+        }
     }
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
@@ -39,7 +46,10 @@ __device__ __forceinline__ u32x2 to_fp8(const float (&x)[8], uint32_t& exponent)
     const float scale = exp2_of_biased(254 - e);
     float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (__builtin_bit_cast(uint32_t, x[i]) & 0x7F800000u) == 0x7F800000u ? __builtin_nanf("") : x[i] * scale;
+    for (int i = 0; i < 8; ++i) y[i] = x[i] * scale;
+    if (odd)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = (__builtin_bit_cast(uint32_t, x[i]) & 0x7F800000u) == 0x7F800000u ? __builtin_nanf("") : y[i];
     u32x2 code;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
