@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
         auto fold = [&](const lora_bf16* gamma, float (&cg)[8], float (&sg)[8]) {
             const u32x4 raw = gamma_of(gamma, ln);
             unpack8(raw, g);
-            others(ln, raw, o);
+            others<!INTER && GL == 32>(ln, raw, o);
 #pragma unroll
             for (int i = 0; i < 8; ++i) { cg[i] = c[i] * g[i]; sg[i] = s[i] * o[i]; }
         };
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_fwd_kernel(RopeArgs p) {
                 if (pass >= passes) break;
                 float x[8], o[8], y[8], sum = 0.f;
                 unpack8(raw[u], x);
-                others(ln, raw[u], o);
+                others<!INTER && GL == 32>(ln, raw[u], o);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
                 const float inv = 1.f / sqrtf(sum_over_head<GL>(sum) / (float)p.D + p.eps);
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(64 * rope_bwd_waves(GL), rope_bwd_waves(GL)) r
                     float x[8], e[8], o[8], sxx = 0.f, sux = 0.f;
                     unpack8(xr[u], x);
                     unpack8(dr[u], e);
-                    others(ln, dr[u], o);
+                    others<!INTER>(ln, dr[u], o);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         e[i] = e[i] * c[i] - o[i] * s[i];

@@ -11,6 +11,7 @@ struct RopeLane {
     bool active, turned;               // ... has entries; they are in the rotated part
     int at, other;                     // first index into a row of the tables; wave lane with the other entries of this one's pairs
     float sign;                        // of the sine in y: - for the first entry of a pair
+    uint32_t even, odd;                // bytes of a word of two entries that hold the other entry of the even and of the odd one's pair (v_perm_b32: 0x0c is a zero)
     __device__ __forceinline__ RopeLane(int D, int rot) {
         const int l = threadIdx.x & 63;
         j = l % GL;
@@ -21,6 +22,8 @@ struct RopeLane {
         at = INTER ? 4 * j : first ? 8 * j : 8 * j - rot / 2;
         other = INTER || !turned ? l : first ? l + rot / 16 : l - rot / 16;
         sign = first ? -1.f : 1.f;
+        even = !turned ? 0x0c0c0c0cu : INTER ? 0x03020c0cu : 0x01000c0cu;
+        odd = !turned ? 0x0c0c0c0cu : INTER ? 0x01000c0cu : 0x03020c0cu;
     }
 };
 
@@ -31,11 +34,11 @@ __device__ __forceinline__ float sum_over_head(float v) {
     return v;
 }
 
-// Cosine and (signed) sine of each of a lane's entries.
+// Cosine and (signed) sine of each of a lane's entries.  Entries that are not turned: 1 and -0, which times the 0 that others() gives them adds nothing, not even to a -0.
 template <int GL, bool INTER, class Args>
 __device__ __forceinline__ void angles(const Args& p, const RopeLane<GL, INTER>& ln, int pos, bool known, float (&c)[8], float (&s)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { c[i] = 1.f; s[i] = 0.f; }
+    for (int i = 0; i < 8; ++i) { c[i] = 1.f; s[i] = -0.f; }
     if (!ln.turned || !known) return;
     const float* cr = p.cos_ + (int64_t)pos * (p.rot / 2) + ln.at;
     const float* sr = p.sin_ + (int64_t)pos * (p.rot / 2) + ln.at;
@@ -50,17 +53,25 @@ __device__ __forceinline__ void angles(const Args& p, const RopeLane<GL, INTER>&
     }
 }
 
-// The other entries of this lane's pairs.
-template <int GL, bool INTER>
+// The other entries of this lane's pairs; zeros where nothing is turned (0 times an infinity that stands there would be NaN): by the lane's selectors at no instruction more, or,
+// SELECTED, where there is no register for those, by a select for two entries.
+template <bool SELECTED = false, int GL, bool INTER>
 __device__ __forceinline__ void others(const RopeLane<GL, INTER>& ln, u32x4 raw, float (&o)[8]) {
-    if constexpr (INTER) {
+    if constexpr (!INTER)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = raw[i] >> 16 | raw[i] << 16;
+        for (int i = 0; i < 4; ++i) raw[i] = (uint32_t)__shfl((int)raw[i], ln.other);
+    if constexpr (SELECTED) {
+        static_assert(!INTER, "the entries of a word change places by the selectors");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = ln.turned ? raw[i] : 0u;
+        unpack8(raw, o);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = __shfl(raw[i], ln.other);
+        for (int i = 0; i < 4; ++i) {
+            o[2 * i] = __builtin_bit_cast(float, __builtin_amdgcn_perm(raw[i], raw[i], ln.even));
+            o[2 * i + 1] = __builtin_bit_cast(float, __builtin_amdgcn_perm(raw[i], raw[i], ln.odd));
+        }
     }
-    unpack8(raw, o);
 }
 
 template <int GL, bool INTER>

@@ -211,3 +211,51 @@ def test_a_launch_and_another(form):
     kref, kbound = _ref(sk, gk, cos, sin, at, False)
     _compare(form, cache, slots[rows.cuda()].cpu(), kref, kbound, sv, form)
     assert int((out[20:(1 << 24) - 20] != 0).sum()) == 0            # (zeros of either sign: 0 x a negative cosine)
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("form", ["bf16", "fp8", "fp4"])
+def test_entries_past_the_rotation_stand_alone(form, inter, norm):
+    """Entries that are not turned have no pair: infinity and NaN there leave the others as they are, and without a norm come out as they went in."""
+    M, H, G, D, rot = 5, 3, 2, 64, 32
+    qkv, q, k, v, gq, gk, cos, sin, pos, slots, cache = _setup(M, H, G, D, rot, 16, form, norm, 77)
+    for x in (q, k):
+        x[0, 1, 41], x[1, 0, 40], x[1, 0, 55], x[2, 1, 63] = float("inf"), -float("inf"), float("inf"), float("nan")
+        x[3, 0, 36], x[3, 0, 37] = 0.0, -0.0
+    dq, dk, dv = (t.cuda().contiguous() for t in (q, k, v))
+    out = binding.lora_kv_cache_append(cache, dq, dk, dv, cos.cuda(), sin.cuda(), pos.cuda(), slots.cuda(), gq=None if gq is None else gq.cuda(),
+                                       gk=None if gk is None else gk.cuda(), eps=EPS, interleaved=inter).cpu()
+
+    def close(got, x, gamma):
+        ref, _ = _ref(x, gamma, cos, sin, pos, inter)
+        top = torch.where(torch.isfinite(x), x.abs(), torch.zeros_like(x)).to(F64).amax(-1, keepdim=True)
+        bound = U16 * ref.abs() + 8 * U32 * top
+        if gamma is not None:
+            clean = torch.where(torch.isfinite(x).all(-1, keepdim=True), x, torch.zeros_like(x))
+            bound = _ref(clean, gamma, cos, sin, pos, inter)[1]             # (beside infinity: 0, exactly; beside NaN: NaN)
+        within(got, ref, bound, (form, inter, norm))
+        if gamma is None:
+            past, held = x[..., rot:], got[..., rot:]
+            assert torch.equal(torch.isnan(past), torch.isnan(held)) and torch.equal(past[~torch.isnan(past)], held[~torch.isnan(past)])
+        return ref
+
+    close(out, q, gq)
+    hk, _, ke, _ = _held(cache, slots)
+    if form == "bf16":
+        close(hk, k, gk)
+        return
+    ref, _ = _ref(k, gk, cos, sin, pos, inter)
+    if form == "fp4":
+        rc, re = quantised4(ref)
+        assert torch.equal(ke, re) and torch.equal(widened4(hk, ke)[ke.repeat_interleave(32, -1) != 255], widened4(rc, re)[re.repeat_interleave(32, -1) != 255])
+        return
+    fine = torch.isfinite(ref)
+    x = torch.where(fine, ref, torch.zeros_like(ref))
+    top = x.abs().amax(-1)
+    e = torch.where(top > 0, torch.ceil(torch.log2(top / 448.0)), torch.zeros_like(top)).clamp(min=-117)
+    a = x / torch.exp2(e)[..., None]
+    step = torch.exp2(torch.floor(torch.log2(a.abs().clamp(min=2.0 ** -6))) - 3)
+    codes = hk.view(torch.float8_e4m3fn).to(F64)
+    assert torch.equal(ke.to(F64), e + 127)
+    assert torch.equal(torch.isnan(codes), ~fine) and torch.equal(codes[fine], (torch.round(a / step) * step)[fine])

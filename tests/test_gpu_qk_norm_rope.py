@@ -185,3 +185,25 @@ def test_most_rows():
         for rows in y.split(some * 4000):
             n = rows.shape[0] // some * some
             assert bool((rows[:n].view(-1, some, D) == y[:some, 0]).all()) and torch.equal(rows[n:], y[:rows.shape[0] - n])
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_entries_past_the_rotation_have_no_pair(inter):
+    """An infinity in an entry that is not turned: the head's others are 0 (a norm over infinity), in its gradient dgamma of that entry alone is not finite."""
+    M, H, G, D, rot = 6, 4, 2, 64, 32
+    _, q, k, gq, gk, cos, sin, pos = _inputs(M, H, G, D, rot, 13)
+    q, k = q.clone(), k.clone()
+    q[2, 1, 40], k[4, 1, 63] = float("inf"), -float("inf")
+    got = binding.lora_qk_norm_rope_fwd(*(t.contiguous().cuda() for t in (q, k, gq, gk, cos, sin, pos)), interleaved=inter)
+    for y, x, gamma in zip(got, (q, k), (gq, gk)):
+        ref = norm_rope(x.to(F64), gamma.to(F64), cos, sin, pos, 1e-6, inter)[0]
+        assert torch.equal(torch.isfinite(y).cpu(), torch.isfinite(ref))
+        hit = torch.isinf(x).any(-1)
+        assert not y.cpu()[hit][torch.isfinite(ref)[hit]].any()
+    _, q, k, *_ = _inputs(M, H, G, D, rot, 13)
+    g = gen(2)
+    dq_out, dk_out = normal(g, (M, H, D)), normal(g, (M, G, D))
+    dq_out[1, 2, 41], dk_out[3, 0, 62] = float("inf"), -float("inf")
+    _, _, dgq, dgk = binding.lora_qk_norm_rope_bwd(*(t.contiguous().cuda() for t in (q, k, gq, gk, cos, sin, pos, dq_out, dk_out)), interleaved=inter)
+    for dg, entry in ((dgq, 41), (dgk, 62)):
+        assert (~torch.isfinite(dg)).nonzero().flatten().tolist() == [entry]
