@@ -310,7 +310,7 @@ lora_status lora_requests_fwd(const lora_bf16* X, const lora_bf16* W, const lora
  * for the H query heads and G key heads (D entries each) of M rows; gamma_q, gamma_k [D].  R turns the pairs (i, i + rot/2), or with
  * interleaved != 0 (2i, 2i+1), of the first rot entries by the angle whose cosine and sine stand in row pos[row] of cos_table,
  * sin_table [positions, rot/2] (fp32); pos [M] is a device array.  A row whose position is outside the tables gets zeros.
- * D: multiples of 16 up to 256; rot: multiples of 16 up to D; H, G up to 1024; M < 2^26; eps > 0.  The output may be the input. */
+ * D: multiples of 16 up to 256; rot: multiples of 16 up to D; H, G up to 1024; M < 2^26; eps > 0.  An output may be its input, with the input's stride. */
 lora_status lora_qk_norm_rope_fwd(const lora_bf16* q, const lora_bf16* k, const lora_bf16* gamma_q, const lora_bf16* gamma_k,
                                   const float* cos_table, const float* sin_table, const int32_t* pos, int64_t M, int32_t H, int32_t G, int32_t D,
                                   int32_t rot, int64_t positions, int64_t ldq, int64_t ldk, int64_t ldqo, int64_t ldko, float eps,
@@ -373,7 +373,7 @@ lora_status lora_kv_cache_read(const lora_kv_cache* cache, const int64_t* slots,
 /* lora_qk_norm_rope_fwd and lora_kv_cache_write in one pass: the normalised and turned queries go to q_out [M,H,dim], the keys and v [M,heads,dim] to their slots.
  * gamma_q and gamma_k NULL (both): no norm, the rotation alone; eps is checked all the same.  Keys that the cache holds in fewer bits are formed in 64 bits and rounded
  * once, to its codes (what is past the range of fp32 counts as not finite); everything else is as in those two calls, a row outside the tables: zeros for query
- * and keys, a slot outside the cache: left out.  q_out may be q.  dim, rot, H and M as in the first. */
+ * and keys, a slot outside the cache: left out.  q_out may be q, with its stride.  dim, rot, H and M as in the first. */
 lora_status lora_kv_cache_append(const lora_kv_cache* cache, const lora_bf16* q, const lora_bf16* k, const lora_bf16* v, const lora_bf16* gamma_q,
                                  const lora_bf16* gamma_k, const float* cos_table, const float* sin_table, const int32_t* pos, const int64_t* slots, int64_t M,
                                  int32_t H, int32_t rot, int64_t positions, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, float eps, int interleaved,

@@ -17,6 +17,8 @@ inline size_t align_up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
 
 // Heads side by side in rows `ld` elements apart.
 inline bool bad_stride(int64_t ld, int64_t heads, int64_t dim) { return ld < heads * dim || (ld & 7) || ld >= (1ll << 31); }
+// Rows written over rows that other waves still read: an output that is the input has its stride.
+inline bool rows_cross(const void* in, const void* out, int64_t ld, int64_t ldo, int64_t M) { return in == out && ld != ldo && M > 1; }
 
 lora_status check_heads(int64_t M, int32_t H, int32_t G, int32_t D) {
     if (M < 0 || H < 1 || G < 1 || D < 1) return LORA_ERR_SHAPE;
@@ -108,6 +110,7 @@ lora_status lora_qk_norm_rope_fwd(const lora_bf16* q, const lora_bf16* k, const 
     if (st != LORA_OK) return st;
     if (!gamma_q || !gamma_k || (positions && (!cos_table || !sin_table)) || (M > 0 && (!q || !k || !pos || !q_out || !k_out))) return LORA_ERR_NULL;
     if (bad_stride(ldq, H, D) || bad_stride(ldqo, H, D) || bad_stride(ldk, G, D) || bad_stride(ldko, G, D)) return LORA_ERR_SHAPE;
+    if (rows_cross(q, q_out, ldq, ldqo, M) || rows_cross(k, k_out, ldk, ldko, M)) return LORA_ERR_SHAPE;
     if (misaligned(q) || misaligned(k) || misaligned(gamma_q) || misaligned(gamma_k) || misaligned(cos_table) || misaligned(sin_table) ||
         misaligned(pos, 4) || misaligned(q_out) || misaligned(k_out))
         return LORA_ERR_ALIGN;
@@ -180,6 +183,7 @@ lora_status lora_kv_cache_append(const lora_kv_cache* cache, const lora_bf16* q,
     if (st != LORA_OK) return st;
     if (!gamma_q != !gamma_k || (positions && (!cos_table || !sin_table)) || (M > 0 && (!q || !k || !v || !pos || !slots || !q_out))) return LORA_ERR_NULL;
     if (bad_stride(ldq, H, a.c.D) || bad_stride(ldqo, H, a.c.D) || bad_stride(ldk, a.c.heads, a.c.D) || bad_stride(ldv, a.c.heads, a.c.D)) return LORA_ERR_SHAPE;
+    if (rows_cross(q, q_out, ldq, ldqo, M)) return LORA_ERR_SHAPE;
     if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(gamma_q) || misaligned(gamma_k) || misaligned(cos_table) || misaligned(sin_table) ||
         misaligned(pos, 4) || misaligned(slots, 8) || misaligned(q_out))
         return LORA_ERR_ALIGN;

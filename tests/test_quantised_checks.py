@@ -111,3 +111,16 @@ def test_workspace_of_smaller_steps(lib):
         T2 = log(1, min(T, B2 * new2))
         big, small = (lib.lora_paged_attn_workspace_bytes(cache, t, G * group, b, n, k, window) for t, b, n, k in ((T, B, new, kv), (T2, B2, new2, kv2)))
         assert 256 <= small <= big, (G, group, (T, B, new, kv), (T2, B2, new2, kv2), window)
+
+
+def test_in_place_with_another_stride(lib):
+    """Rows written over rows that are still read are refused: queries (and keys) in place keep their stride."""
+    p, other = P(0x1000), P(0x800000)
+    base = dict(gq=p, gk=p, cos=p, sin=p, pos=p)
+    append = dict(cache=_cache(), q=p, k=other, v=other, **base, slots=p, M=4, H=4, rot=64, positions=10, ldq=512, ldk=128, ldv=128, ldqo=256, eps=1e-6, inter=0, qo=p,
+                  stream=None)
+    f = lambda **kw: lib.lora_kv_cache_append(*_changed(append, **kw))
+    assert f() == SHAPE and f(ldq=256, ldqo=512) == SHAPE and f(M=0) == OK and f(M=0, ldqo=512) == OK
+    rope = dict(q=p, k=other, **base, M=4, H=4, G=2, D=64, rot=64, positions=10, ldq=512, ldk=128, ldqo=512, ldko=128, eps=1e-6, inter=0, qo=p, ko=other, stream=None)
+    f = lambda **kw: lib.lora_qk_norm_rope_fwd(*_changed(rope, **kw))
+    assert f(ldqo=256) == SHAPE and f(ldko=256) == SHAPE and f(ldqo=256, M=0) == OK
