@@ -343,6 +343,14 @@ lora_status lora_weights_read(const uint8_t* codes, const uint8_t* exps, int64_t
 lora_status lora_requests_quantised_fwd(const lora_bf16* X, const uint8_t* codes, const uint8_t* exps, const lora_bf16* A, const lora_bf16* B,
                                         const int32_t* ids, const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P,
                                         lora_bf16* Y, lora_bf16* S, lora_stream stream);
+/* Diagnostic (host only): what lora_requests_quantised_fwd runs with for these sizes.  The same call gives the same bits; the same row in another batch need not: the tile goes
+ * by M, K and N, S by the other rows' adapters too, and each sums in an order of its own. */
+typedef struct {
+    int32_t rows, columns;    /* output tile of a workgroup */
+    int32_t ring_blocks;      /* blocks of 128 of the contraction that its rings hold at once */
+    int32_t own_term;         /* 1: S is formed in the same launch, by every workgroup; 0: in a launch of its own, or there are no adapters */
+} lora_quantised_tiles;
+lora_status lora_debug_quantised_tiles(int64_t M, int64_t K, int64_t N, int32_t r, int64_t P, lora_quantised_tiles* out);
 
 /* A paged cache of keys and values (the caller's device memory): k, v [pages, heads, page, dim].  fp8 == 0: lora_bf16.  fp8 == LORA_KV_FP4: 4 bits, k, v
  * [pages, heads, page, dim/2] bytes, k_exp, v_exp [pages, heads, page, dim/32], dim a multiple of 32.  Any other fp8: e4m3

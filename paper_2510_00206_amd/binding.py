@@ -23,7 +23,7 @@ EXPORTS = ("lora_fwd", "lora_bwd", "lora_bwd_noalloc", "multi_lora_fwd", "multi_
            "lora_unfused_fwd", "lora_unfused_bwd", "lora_unfused_workspace_bytes",
            "lora_requests_fwd", "lora_qk_norm_rope_fwd", "lora_qk_norm_rope_bwd", "lora_qk_norm_rope_workspace_bytes",
            "lora_kv_cache_write", "lora_kv_cache_read", "lora_paged_attn_fwd", "lora_paged_attn_workspace_bytes",
-           "lora_weights_write", "lora_weights_read", "lora_requests_quantised_fwd", "lora_kv_cache_append")
+           "lora_weights_write", "lora_weights_read", "lora_requests_quantised_fwd", "lora_debug_quantised_tiles", "lora_kv_cache_append")
 
 _lib = None
 
@@ -43,6 +43,11 @@ class Launches(C.Structure):
     """What operations (1), (2) and (5) launch (lora_launches in the header)."""
     _fields_ = [(f, C.c_int32) for f in ("down_rows", "down_parts", "down_ring")] + \
                [("down_workgroups", C.c_int64), ("fwd", GemmLaunch * 2), ("dx", GemmLaunch * 2)]
+
+
+class QuantisedTiles(C.Structure):
+    """What lora_requests_quantised_fwd runs with (lora_quantised_tiles in the header)."""
+    _fields_ = [(f, C.c_int32) for f in ("rows", "columns", "ring_blocks", "own_term")]
 
 
 class CacheArrays(C.Structure):
@@ -115,13 +120,15 @@ def load_library() -> C.CDLL:
     lib.lora_weights_write.argtypes = [P, I64, I64, P, P, P]
     lib.lora_weights_read.argtypes = [P, P, I64, I64, P, P]
     lib.lora_requests_quantised_fwd.argtypes = [P] * 8 + [I64, I64, I64, I32, I64, P, P, P]
+    lib.lora_debug_quantised_tiles.argtypes = [I64, I64, I64, I32, I64, C.POINTER(QuantisedTiles)]
     lib.lora_kv_cache_append.argtypes = [CA] + [P] * 9 + [I64, I32, I32, I64, I64, I64, I64, I64, F, C.c_int, P, P]
     lib.lora_paged_attn_fwd.argtypes = [P, CA, P, P, P, I64, I32] + [I64] * 7 + [F, I32, P, P, SZ, P]
     lib.lora_paged_attn_workspace_bytes.argtypes = [CA, I64, I32, I64, I64, I64, I32]
     for f in ("lora_qk_norm_rope_workspace_bytes", "lora_paged_attn_workspace_bytes"):
         getattr(lib, f).restype = SZ
     for f in ("lora_requests_fwd", "lora_qk_norm_rope_fwd", "lora_qk_norm_rope_bwd", "lora_kv_cache_write", "lora_kv_cache_read",
-              "lora_paged_attn_fwd", "lora_weights_write", "lora_weights_read", "lora_requests_quantised_fwd", "lora_kv_cache_append"):
+              "lora_paged_attn_fwd", "lora_weights_write", "lora_weights_read", "lora_requests_quantised_fwd", "lora_debug_quantised_tiles",
+              "lora_kv_cache_append"):
         getattr(lib, f).restype = C.c_int
     for f in ("lora_fwd", "lora_bwd", "multi_lora_fwd", "multi_lora_bwd", "multi_lora_fwd_ranked",
               "multi_lora_bwd_ranked", "lora_debug_mask",
@@ -446,6 +453,13 @@ def lora_requests_quantised_fwd(X, codes, exps, A=None, B=None, ids=None, s=None
                                                       None if ranks is None else _at(ranks, _I32), _at(s, _F32), M, K, N, r, P, _at(Y, _BF16),
                                                       _at(S, _BF16), _stream()))
     return Y, S
+
+
+def lora_debug_quantised_tiles(M, K, N, r=0, P=0) -> QuantisedTiles:
+    """What lora_requests_quantised_fwd of these sizes runs with (host only)."""
+    out = QuantisedTiles()
+    _check(load_library().lora_debug_quantised_tiles(M, K, N, r, P, C.byref(out)))
+    return out
 
 
 def _rope_sizes(q, k, gq, gk, cos, sin, pos):

@@ -111,12 +111,14 @@ __device__ __forceinline__ int half_exp_byte(int r, int c, int q) { return 4 * r
 // to a ring of the 16 x 32 tiles instead of two, which is all that LDS holds: the same.
 template <int XC_, int NI_, int NW_, int TW_, int D_>
 struct FewLayer {
+    static constexpr bool FEW = true;
     static constexpr int XC = XC_, NI = NI_, NW = NW_, TW = TW_, D = D_, TN = 16 * NI;
     struct Term {                      // of one wave
         static constexpr int MI = 1, NI = NI_, NW = NW_, CW = TW_, LDS = 160 * 1024, TN = 16 * NI_, SUBS = 0, EVERY = TW_, HELD = 0;
         static constexpr bool AHEAD = false;
     };
     static constexpr int SLOT = XC * 1024 + BlockCopies<XC, NI, true>::PART;
+    static constexpr int TM = 16, RING_BLOCKS = NW * D;
     static constexpr int RING = NW * D * SLOT, SUMS = (NW + TW) * NI * 1024, BODY = RING > SUMS ? RING : SUMS;
     static constexpr int LDS = BODY + TW * (int)sizeof(RequestList<Term>);
     static_assert((XC + NI + 2) * (D - 1) < 64 && LDS <= 160 * 1024, "the wait counter; a compute unit's LDS");
@@ -276,6 +278,7 @@ __global__ void __launch_bounds__(64 * (C::NW + (FORM != Few::plain ? C::TW : 0)
 // time, 95 MB in pieces of 64 bytes.
 template <int MI_, int NI_, int WM_, int WN_, int NS_, int CW_>
 struct RingLayer {
+    static constexpr bool FEW = false;
     static constexpr int MI = MI_, NI = NI_, WM = WM_, WN = WN_, NS = NS_, CW = CW_, NW = WM * WN, THREADS = 64 * NW;
     static constexpr int TM = 16 * MI * WM, TN = 16 * NI * WN;
     static constexpr int XB = TM * 2 * kBlock, XC = XB / 1024 / CW, RW = TN / CW, CC = RW / 16;     // a block's X, then the parts of the copying waves
@@ -287,6 +290,7 @@ struct RingLayer {
         static constexpr int HELD = (MI_ - MI) * NI * 4;                            // the other rows' accumulators
         static constexpr bool AHEAD = false;
     };
+    static constexpr int RING_BLOCKS = NS;
     static constexpr int RING = NS * STAGE > OUT ? NS * STAGE : OUT;
     static constexpr int LDS = RING + NW * (int)sizeof(RequestList<Term>);
     static_assert(XB % (1024 * CW) == 0 && XC <= 8 && RW % 16 == 0 && RW <= 64, "copies of a block: whole, in reach of the immediates");
@@ -493,17 +497,18 @@ static hipError_t launch_layer(const LayerArgs& a, int tile_rows, int tile_colum
     });
 }
 
-template <class C, bool OWN>
-static hipError_t launch_few(const LayerArgs& a, hipStream_t st) {
-    if constexpr (OWN)
-        if (a.S) return launch_layer<layer_few_kernel<C, Few::own>>(a, 16, C::TN, 64 * (C::NW + C::TW), C::LDS, st);
-    if (a.t.P > 0) return launch_layer<layer_few_kernel<C, Few::term>>(a, 16, C::TN, 64 * (C::NW + C::TW), C::LDS, st);
-    return launch_layer<layer_few_kernel<C, Few::plain>>(a, 16, C::TN, 64 * C::NW, C::LDS, st);
-}
 template <class C>
-static hipError_t launch_ring(const LayerArgs& a, hipStream_t st) {
-    if (a.t.P > 0) return launch_layer<layer_ring_kernel<C, true>>(a, C::TM, C::TN, C::THREADS + 64 * C::CW, C::LDS, st);
-    return launch_layer<layer_ring_kernel<C, false>>(a, C::TM, C::TN, C::THREADS + 64 * C::CW, C::LDS, st);
+static hipError_t launch_kind(const LayerArgs& a, bool own, hipStream_t st) {
+    if constexpr (C::FEW) {
+        constexpr int THREADS = 64 * (C::NW + C::TW);
+        if constexpr (C::XC == 1)
+            if (own) return launch_layer<layer_few_kernel<C, Few::own>>(a, 16, C::TN, THREADS, C::LDS, st);
+        if (a.t.P > 0) return launch_layer<layer_few_kernel<C, Few::term>>(a, 16, C::TN, THREADS, C::LDS, st);
+        return launch_layer<layer_few_kernel<C, Few::plain>>(a, 16, C::TN, 64 * C::NW, C::LDS, st);
+    } else {
+        if (a.t.P > 0) return launch_layer<layer_ring_kernel<C, true>>(a, C::TM, C::TN, C::THREADS + 64 * C::CW, C::LDS, st);
+        return launch_layer<layer_ring_kernel<C, false>>(a, C::TM, C::TN, C::THREADS + 64 * C::CW, C::LDS, st);
+    }
 }
 
 // Rows and columns of a workgroup, and what a block of the contraction takes it, us, while there is one on a compute unit; 2.5 a round beside them (fitted to 1 - 2048
@@ -526,14 +531,36 @@ static int choose_kind(int M, int K, int N) {
     return best;
 }
 
+// f(kind): of the layer over these rows.
+template <class F>
+static auto with_kind(int M, int K, int N, F&& f) {
+    switch (choose_kind(M, K, N)) {
+        case 0: return M <= 4 ? f(FewLayer<1, 1, 8, 4, 4>{}) : f(FewLayer<4, 1, 8, 4, 3>{});
+        case 1: return f(FewLayer<4, 2, 8, 4, 2>{});
+        case 2: return f(FewLayer<4, 4, 8, 4, 2>{});
+        case 3: return f(RingLayer<1, 2, 2, 2, 6, 1>{});
+        case 4: return f(RingLayer<2, 2, 2, 2, 7, 2>{});
+        case 5: return f(RingLayer<4, 2, 1, 4, 6, 2>{});
+        case 6: return f(RingLayer<4, 4, 1, 4, 4, 4>{});
+        default: return f(RingLayer<8, 4, 1, 4, 3, 4>{});
+    }
+}
+
+// S formed by every workgroup for itself (own_term), where its rows' columns are few and short enough.  us in a captured graph (with the call from Python), two
+// launches / one: one row of r = 16, 1024 -> 1024 5.7 / 3.9 (9.6 / 7.3), 4096 -> 4096 7.5 / 6.8 (9.7 / 7.3), 8192 -> 2048 9.8 / 10.1; of 32, 1024 -> 1024 5.8 / 4.7,
+// 2048 -> 4096 6.5 / 7.1; of 64, 256 -> 256 5.8 / 5.6, 1024 -> 1024 6.1 / 6.3; two of 16, 1024 -> 1024 6.0 / 5.0, 2048 -> 4096 6.5 / 7.3.  (With wider tiles, N = 14336, it was
+// never faster: 12.2 / 18.2 for one row of 4096.)
+static bool forms_own_term(int M, int K, int N, int r, int P) {
+    const int64_t columns = (int64_t)M * r;
+    return P > 0 && M <= 4 && choose_kind(M, K, N) == 0 && columns * columns * K <= 1 << 20;
+}
+
+QuantisedTiles quantised_tiles(int M, int K, int N, int r, int P) {
+    return with_kind(M, K, N, [&](auto c) { return QuantisedTiles{c.TM, c.TN, c.RING_BLOCKS, forms_own_term(M, K, N, r, P)}; });
+}
+
 hipError_t launch_quantised_requests(const QuantisedRequestArgs& a, hipStream_t st) {
-    const int kind = choose_kind(a.r.M, a.r.K, a.r.N);
-    // S formed by every workgroup for itself (own_term), where its rows' columns are few and short enough.  us in a captured graph (with the call from Python), two
-    // launches / one: one row of r = 16, 1024 -> 1024 5.7 / 3.9 (9.6 / 7.3), 4096 -> 4096 7.5 / 6.8 (9.7 / 7.3), 8192 -> 2048 9.8 / 10.1; of 32, 1024 -> 1024 5.8 / 4.7,
-    // 2048 -> 4096 6.5 / 7.1; of 64, 256 -> 256 5.8 / 5.6, 1024 -> 1024 6.1 / 6.3; two of 16, 1024 -> 1024 6.0 / 5.0, 2048 -> 4096 6.5 / 7.3.  (With wider tiles, N = 14336, it was
-    // never faster: 12.2 / 18.2 for one row of 4096.)
-    const int64_t columns = (int64_t)a.r.M * a.r.r;
-    const bool own = a.r.P > 0 && kind == 0 && a.r.M <= 4 && columns * columns * a.r.K <= 1 << 20;
+    const bool own = forms_own_term(a.r.M, a.r.K, a.r.N, a.r.r, a.r.P);
     const hipError_t e = a.r.P > 0 && !own ? launch_request_down(a.r, st) : hipSuccess;
     if (e != hipSuccess) return e;
     LayerArgs g{};
@@ -555,16 +582,7 @@ hipError_t launch_quantised_requests(const QuantisedRequestArgs& a, hipStream_t 
         g.s = a.r.s;
         g.S = a.r.S;
     }
-    switch (kind) {
-        case 0: return a.r.M <= 4 ? launch_few<FewLayer<1, 1, 8, 4, 4>, true>(g, st) : launch_few<FewLayer<4, 1, 8, 4, 3>, false>(g, st);
-        case 1: return launch_few<FewLayer<4, 2, 8, 4, 2>, false>(g, st);
-        case 2: return launch_few<FewLayer<4, 4, 8, 4, 2>, false>(g, st);
-        case 3: return launch_ring<RingLayer<1, 2, 2, 2, 6, 1>>(g, st);
-        case 4: return launch_ring<RingLayer<2, 2, 2, 2, 7, 2>>(g, st);
-        case 5: return launch_ring<RingLayer<4, 2, 1, 4, 6, 2>>(g, st);
-        case 6: return launch_ring<RingLayer<4, 4, 1, 4, 4, 4>>(g, st);
-        default: return launch_ring<RingLayer<8, 4, 1, 4, 3, 4>>(g, st);
-    }
+    return with_kind(a.r.M, a.r.K, a.r.N, [&](auto c) { return launch_kind<decltype(c)>(g, own, st); });
 }
 
 }  // namespace lf

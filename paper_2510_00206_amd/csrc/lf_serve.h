@@ -73,6 +73,7 @@ struct RequestArgs {
     int M, K, N, r, P;
 };
 struct QuantisedRequestArgs { RequestArgs r; const uint8_t* codes; const uint8_t* exps; };     // r.P == 0: no adapters
+struct QuantisedTiles { int rows, columns, ring_blocks; bool own_term; };
 
 int rope_blocks(int64_t M, int H, int G, int D);        // of the backward: planes of partial sums
 hipError_t launch_rope_fwd(RopeArgs a, bool interleaved, hipStream_t st);
@@ -87,6 +88,7 @@ int64_t attn_part_rows(int64_t T, int B, int G, int group, int max_new, int64_t 
 hipError_t launch_attn(AttnArgs a, const AttnPlan& p, int max_new, hipStream_t st);
 hipError_t launch_request_down(const RequestArgs& a, hipStream_t st);       // S alone
 hipError_t launch_requests(const RequestArgs& a, hipStream_t st);
+QuantisedTiles quantised_tiles(int M, int K, int N, int r, int P);
 hipError_t launch_quantised_requests(const QuantisedRequestArgs& a, hipStream_t st);
 
 // ---- device pieces ------------------------------------------------------------------------------

@@ -75,6 +75,12 @@ lora_status check_weights(const void* W, const void* codes, const void* exps, in
     return LORA_OK;
 }
 
+lora_status check_quantised(int64_t M, int64_t K, int64_t N, int32_t r, int64_t P) {
+    if (M < 0 || K <= 0 || N <= 0 || M >= (1ll << 31) || K >= (1ll << 31) || N >= (1ll << 31) || P < 0 || P >= (1ll << 31)) return LORA_ERR_SHAPE;
+    if ((K & 63) || (N & 63) || K > (1 << 22) || N > (1 << 22) || (P > 0 && !(r == 16 || r == 32 || r == 64)) || M >= (1 << 21)) return LORA_ERR_UNSUPPORTED;
+    return LORA_OK;
+}
+
 lora_status check_attn(const PagedCache& c, int64_t T, int32_t H, int64_t B, int64_t max_new, int64_t max_kv, int32_t window) {
     if (T < 0 || B < 0 || H < 1 || max_new < 0 || max_kv < 0 || window < 0 || H % c.heads) return LORA_ERR_SHAPE;
     const int64_t most = 0x7FFFFFFF / H;                   // (T * H could wrap)
@@ -163,14 +169,23 @@ lora_status lora_weights_read(const uint8_t* codes, const uint8_t* exps, int64_t
 lora_status lora_requests_quantised_fwd(const lora_bf16* X, const uint8_t* codes, const uint8_t* exps, const lora_bf16* A, const lora_bf16* B,
                                         const int32_t* ids, const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P,
                                         lora_bf16* Y, lora_bf16* S, lora_stream stream) {
-    if (M < 0 || K <= 0 || N <= 0 || M >= (1ll << 31) || K >= (1ll << 31) || N >= (1ll << 31) || P < 0 || P >= (1ll << 31)) return LORA_ERR_SHAPE;
-    if ((K & 63) || (N & 63) || K > (1 << 22) || N > (1 << 22) || (P > 0 && !(r == 16 || r == 32 || r == 64)) || M >= (1 << 21)) return LORA_ERR_UNSUPPORTED;
+    const lora_status st = check_quantised(M, K, N, r, P);
+    if (st != LORA_OK) return st;
     if (!codes || !exps || (M > 0 && (!X || !Y)) || (P > 0 && (!A || !B || !s || (M > 0 && (!ids || !S))))) return LORA_ERR_NULL;
     if (misaligned(X) || misaligned(codes) || misaligned(exps) || misaligned(Y)) return LORA_ERR_ALIGN;
     if (P > 0 && (misaligned(A) || misaligned(B) || misaligned(S) || misaligned(ids, 4) || misaligned(ranks, 4) || misaligned(s, 4))) return LORA_ERR_ALIGN;
     if (M == 0) return LORA_OK;
     return done(launch_quantised_requests(
         QuantisedRequestArgs{RequestArgs{X, nullptr, A, B, ids, ranks, s, Y, S, (int)M, (int)K, (int)N, r, (int)P}, codes, exps}, (hipStream_t)stream));
+}
+
+lora_status lora_debug_quantised_tiles(int64_t M, int64_t K, int64_t N, int32_t r, int64_t P, lora_quantised_tiles* out) {
+    const lora_status st = check_quantised(M, K, N, r, P);
+    if (st != LORA_OK) return st;
+    if (!out) return LORA_ERR_NULL;
+    const QuantisedTiles t = quantised_tiles((int)M, (int)K, (int)N, r, (int)P);
+    *out = M ? lora_quantised_tiles{t.rows, t.columns, t.ring_blocks, t.own_term} : lora_quantised_tiles{};
+    return LORA_OK;
 }
 
 lora_status lora_kv_cache_append(const lora_kv_cache* cache, const lora_bf16* q, const lora_bf16* k, const lora_bf16* v, const lora_bf16* gamma_q,

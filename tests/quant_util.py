@@ -35,3 +35,14 @@ def widened4(codes, exps):
     x = GRID[c % 8] * torch.where(c >= 8, -1.0, 1.0)
     scale = torch.where(exps == 255, torch.full(exps.shape, float("nan"), dtype=F64), torch.ldexp(torch.ones(exps.shape, dtype=F64), exps.int() - 127))
     return (x.unflatten(-1, (-1, 32)) * scale[..., None]).flatten(-2)
+
+
+# Layers whose contraction is more than twice what the rings of their tile hold (tile; rows, contraction, columns): whole blocks of 128, and half a one at the end.
+WRAPPED = [((16, 16), 3, 8320, 64), ((16, 16), 4, 8384, 128), ((16, 16), 13, 6272, 64), ((16, 16), 5, 6336, 192),
+           ((16, 32), 13, 4224, 4160), ((16, 32), 5, 4288, 4224),
+           ((16, 64), 20, 4224, 4160), ((16, 64), 29, 4288, 4224),
+           ((32, 64), 33, 1664, 5504), ((32, 64), 47, 1728, 5504),
+           ((64, 64), 65, 1920, 5504), ((64, 64), 100, 1984, 5568),
+           ((64, 128), 129, 1664, 5504), ((64, 128), 150, 1728, 5568),
+           ((64, 256), 257, 1152, 6592), ((64, 256), 300, 1216, 6656),
+           ((128, 256), 513, 896, 7232), ((128, 256), 600, 960, 7296)]

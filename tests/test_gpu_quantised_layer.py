@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2510_00206_amd import binding
-from quant_util import quantised4, widened4
+from quant_util import WRAPPED, quantised4, widened4
 from serve_util import BF16, U32, U16, F64, gen, normal, requests, within
 
 pytestmark = pytest.mark.gpu
@@ -210,3 +210,25 @@ def test_an_adapter_that_diverged_in_one_launch():
     Y, _ = binding.lora_requests_quantised_fwd(*(t.cuda() for t in (X, codes, exps, A, B, ids, s)))
     bad = ~torch.isfinite(Y.cpu())
     assert bool(bad[1, 7]) and int(bad.sum()) == 1 and torch.equal(Y.cpu()[~bad], want[~bad])
+
+
+@pytest.mark.parametrize("P", [0, 5])
+@pytest.mark.parametrize("tile,M,K,N", WRAPPED)
+def test_rings_that_wrap(tile, M, K, N, P):
+    """Every kind of tile over contractions of more than twice what its rings hold, so that every place is filled again and again and the waits are counted ones."""
+    t = binding.lora_debug_quantised_tiles(M, K, N, 32, P)
+    assert (t.rows, t.columns) == tile and K // 128 > 2 * t.ring_blocks
+    g = gen(M + K)
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, dtype=torch.uint8)
+    exps = torch.randint(118, 123, (N, K // 32), generator=g, dtype=torch.uint8)
+    X = normal(g, (M, K))
+    if P:
+        A, B, s = normal(g, (P, 32, K), K ** -0.5), normal(g, (P, N, 32), 0.1), torch.rand(P, generator=g) * 2 - 0.5
+        ids, ranks = torch.randint(-1, P, (M,), generator=g, dtype=torch.int32), torch.randint(0, 33, (P,), generator=g, dtype=torch.int32)
+        _check((X, codes, exps, A, B, ids, s, ranks), ("wrapped", tile, M, K, N))
+        return
+    print("wrapped, no adapters", tile, M, K, N, flush=True)
+    Y, _ = binding.lora_requests_quantised_fwd(X.cuda(), codes.cuda(), exps.cuda())
+    W = widened4(codes, exps)
+    ref = X.to(F64) @ W.t()
+    within(Y, ref, U16 * ref.abs() + (1 + U16) * K * U32 * (X.to(F64).abs() @ W.abs().t()), (tile, M, K, N))

@@ -124,3 +124,25 @@ def test_in_place_with_another_stride(lib):
     rope = dict(q=p, k=other, **base, M=4, H=4, G=2, D=64, rot=64, positions=10, ldq=512, ldk=128, ldqo=512, ldko=128, eps=1e-6, inter=0, qo=p, ko=other, stream=None)
     f = lambda **kw: lib.lora_qk_norm_rope_fwd(*_changed(rope, **kw))
     assert f(ldqo=256) == SHAPE and f(ldko=256) == SHAPE and f(ldqo=256, M=0) == OK
+
+
+def test_layer_tiles(lib):
+    """The kinds of tile that the layer's tests are meant for are those that these sizes take, and every kind is among them."""
+    from paper_2510_00206_amd import binding
+    from quant_util import WRAPPED
+    seen = set()
+    for tile, M, K, N in WRAPPED:
+        t = binding.lora_debug_quantised_tiles(M, K, N, 32, 5)
+        assert (t.rows, t.columns) == tile and K // 128 > 2 * t.ring_blocks and not t.own_term, (tile, M, K, N, t.rows, t.columns, t.ring_blocks)
+        seen.add((tile, t.ring_blocks, K % 128))
+    for M in list(range(1, 70)) + [80, 100, 130, 200, 260, 300, 520, 700, 1300, 2050]:
+        for K in (64, 256, 1024, 4096, 4160, 14336):
+            for N in (64, 1024, 4096, 4160, 6144, 14336):
+                t = binding.lora_debug_quantised_tiles(M, K, N)
+                assert all(((t.rows, t.columns), t.ring_blocks, half) in seen for half in (0, 64)), (M, K, N)
+    one = [binding.lora_debug_quantised_tiles(1, 1024, 1024, r, P).own_term for r, P in ((16, 4), (32, 4), (64, 4), (16, 0))]
+    assert one == [1, 1, 0, 0]
+    f = lib.lora_debug_quantised_tiles
+    out = binding.QuantisedTiles()
+    assert f(8, 64, 64, 16, 1, None) == NULL and f(-1, 64, 64, 16, 1, C.byref(out)) == SHAPE and f(8, 32, 64, 16, 1, C.byref(out)) == UNSUPPORTED
+    assert f(0, 64, 64, 16, 1, C.byref(out)) == OK and out.rows == out.columns == out.ring_blocks == 0
