@@ -339,7 +339,7 @@ lora_status lora_weights_write(const lora_bf16* W, int64_t N, int64_t K, uint8_t
 lora_status lora_weights_read(const uint8_t* codes, const uint8_t* exps, int64_t N, int64_t K, lora_bf16* W, lora_stream stream);
 
 /* lora_requests_fwd over such weights, without a copy of them in bf16: the arguments are its own, with codes and exps for W.  P = 0: no adapters (A, B, ids, ranks, s, S
- * may be NULL, r anything). */
+ * may be NULL, r anything; S is left as it is). */
 lora_status lora_requests_quantised_fwd(const lora_bf16* X, const uint8_t* codes, const uint8_t* exps, const lora_bf16* A, const lora_bf16* B,
                                         const int32_t* ids, const int32_t* ranks, const float* s, int64_t M, int64_t K, int64_t N, int32_t r, int64_t P,
                                         lora_bf16* Y, lora_bf16* S, lora_stream stream);
@@ -353,7 +353,7 @@ typedef struct {
 lora_status lora_debug_quantised_tiles(int64_t M, int64_t K, int64_t N, int32_t r, int64_t P, lora_quantised_tiles* out);
 
 /* A paged cache of keys and values (the caller's device memory): k, v [pages, heads, page, dim].  fp8 == 0: lora_bf16.  fp8 == LORA_KV_FP4: 4 bits, k, v
- * [pages, heads, page, dim/2] bytes, k_exp, v_exp [pages, heads, page, dim/32], dim a multiple of 32.  Any other fp8: e4m3
+ * [pages, heads, page, dim/2] bytes, k_exp, v_exp [pages, heads, page, dim/32], dim a multiple of 32.  Any other fp8 (any other true value): e4m3
  * bytes, and k_exp, v_exp [pages, heads, page] with the biased exponent of one power of two for every token and head; the value is
  * e4m3 * 2^(exp - 127), exp 10 .. 247 (what a write gives), or less beside codes of zero (a cache cleared to zeros).  page: a power of
  * two, 16 .. 1024 tokens; dim: multiples of 16 up to 256; heads up to 1024.  Written and read: M * heads of 2^27 - 8 and fewer. */

@@ -134,9 +134,11 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs p) {
 }
 
 // Parts of a row.  Queries: of two passes, beside a quantised cache (whose keys take longer) four, and of one in small batches; keys and values: one part, in small batches
-// one to a pass.  us (32 + 2 x 8 heads of 128: eight passes of queries, two of keys), parts of queries / of keys and values 1/1, 2/1, 4/1, 4/2, 8/2: to 4 bits, 16 rows 4.2, 4.2, 4.2,
-// 2.1, 2.1 (beside 2.6 of reading back); 800 rows 6.5, 6.8, 6.8, 5.0, 5.6; 2085 rows 9.4, 8.8, 9.1, 9.5, 11.8; 8192 rows 30.9, 30.7, 35.8, 38.8, 51.8; bf16, 16 rows 6.2, 4.4, 4.2, 3.6,
-// 3.6; 800 rows 8.8, 7.6, 6.8, 6.9, 7.9; 2085 rows 12.4, 12.0, 11.4, 12.3, 13.2; 8192 rows 46.8, 43.8, 43.5, 45.8, 55.2.
+// one to a pass.  us in a captured graph, 32 + 2 x 8 heads of 128 (eight passes of queries, two of keys), parts of queries / of keys and values 1/1, 2/1, 4/1, 4/2, 8/2:
+//   to 4 bits  16 rows 6.9, 6.9, 6.9, 4.8, 4.8;  800 9.4, 9.6, 9.7, 7.9, 8.8;  2085 14.8, 14.5, 14.6, 15.0, 17.2;  8192 46.4, 46.0, 51.2, 53.5, 66.4
+//   to fp8     16 rows 7.3, 7.2, 7.2, 5.0, 5.0;  800 9.9, 10.1, 10.2, 8.1, 8.9;  2085 15.0, 14.5, 14.5, 15.4, 17.4;  8192 47.4, 47.3, 52.1, 54.9, 67.5
+//   bf16       16 rows 6.2, 4.4, 4.2, 3.6, 3.6;  800 8.9, 7.6, 6.8, 7.1, 8.1;  2085 12.8, 12.5, 11.9, 12.5, 14.0;  8192 46.5, 44.1, 44.7, 47.7, 55.4
+// This rule: 4.8, 7.8, 14.3, 46.4; 5.0, 8.1, 14.4, 47.1; 3.6, 7.1, 11.9, 45.1.  (The bf16 kernel with the cache's form a constant in it too: 2085 rows 12.6 instead of 12.0.)
 hipError_t launch_append(AppendArgs a, bool interleaved, hipStream_t st) {
     return with_lanes(a.c.D, [&](auto gl) {
         constexpr int HEADS = 64 / gl(), WAVES = kAppendThreads / 64;

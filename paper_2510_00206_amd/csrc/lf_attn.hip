@@ -169,7 +169,7 @@ __device__ __forceinline__ bool follow(const float (&top)[NQ], float (&m)[NQ], f
 // References past kFar.  p_of takes the scaled score exactly, m is rounded: past 2^24 their difference is no longer near 0 for the largest score itself, and past 2^31
 // its power of two is infinity or 0.  Such a row counts its scores from one of them (base: a float for every query of the wave, in LDS, read
 // where far is set; zero for the other rows) and m from there on, so that the largest score's difference is exact.  Rare: a branch a step on a
-// scalar, and nothing kept in registers (us, without / with: 278 / 278.5 for the chunks below, 343.9 / 344.9 over an fp8 cache, 61.3 / 62.5 for 16 x 6 tokens over
+// scalar, and nothing kept in registers (us, without / with: 278 / 278.5 for the chunks below, 343.9 / 344.9 over an fp8 cache when that took so long, 61.3 / 62.5 for 16 x 6 tokens over
 // up to 9000 keys, fp8, long single tokens level).
 template <int NQ, int KB>
 __device__ __forceinline__ void count_from_base(f32x4 (&s)[NQ][KB], float (&top)[NQ], const float* base, int c) {
@@ -571,9 +571,10 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) attn_few_kernel(AttnArgs
 // tile n + 1, the softmax of tile n and the values of tile n - 1 are one stream of instructions, in which the vector ones stand between the matrix
 // ones, two to each: only those of the same wave run beside a matrix instruction, those of other waves wait for it.  Measured: two
 // prompts' 1021 new tokens over 5003 and 16000 keys, 32 heads of 128 to 8, 250 GFLOP, 265 us, 940 TFLOP/s (a product of 8192^3: 1320); bound by the issue of
-// instructions (a step of 64 keys takes 3300 cycles, of which its 64 matrix instructions and the 64 of the SIMD's other wave 2050).  With the join 280; over 4 bits 330:
-// two waits and two widenings a step.  Codes into registers instead of LDS, widened in one go 345, between the matrix instructions 361 (the registers are
-// all taken); through two places in LDS, between the matrix instructions, 359.
+// instructions (a step of 64 keys takes 3300 cycles, of which its 64 matrix instructions and the 64 of the SIMD's other wave 2050).  With the join 280; over 4 bits 316, over
+// fp8 332: two waits and two widenings a step.  With lane numbers taken for signed ones, whose every division by a power of two is some instructions more, 331 and 348; beside that 331, codes into
+// registers instead of LDS, widened in one go 345, between the matrix instructions 361 (the registers are all taken); through two places in LDS, between the matrix
+// instructions, 359.
 template <int D, int FORM>
 struct Many {
     static constexpr int KEYS = 64, ROWS = 128, NQ = 2;

@@ -104,10 +104,13 @@ __device__ __forceinline__ int exp_byte(bool split, int r, int c, int q) { retur
 __device__ __forceinline__ int half_exp_byte(int r, int c, int q) { return 4 * r + 2 * (c & 1) + (q >> 1); }
 
 // ---- few rows ---------------------------------------------------------------------------------------
-// Bound by the reading of the weights, of which a launch of a few us sees mostly the latency.  A workgroup has up to 16 rows (of which it brings 4 XC) and NI x 16 columns, its NW waves every NW-th block of the contraction, which each brings into a ring of
+// Bound by what a compute unit brings in, of which a launch of a few us sees mostly the latency: X comes again with every tile of columns, beside 1 KB of codes of a 16 x 16 tile's
+// block 4 KB of it (1 KB where there are four rows at most).  Without adapters, in a captured graph, 14336 -> 4096: one row 8.6 us, four 8.5, five 10.3, 16 rows 11.7, 64 rows (16 x 64
+// tiles) 19.9, that is 49 and 47 KB a us and compute unit for the last two; 4096 -> 4096 4.2, 4.4, 4.7, 5.3, 7.8.
+// A workgroup has up to 16 rows (of which it brings 4 XC) and NI x 16 columns, its NW waves every NW-th block of the contraction, which each brings into a ring of
 // its own of D blocks, with no barrier; the adapters' term is formed by TW waves of its own beside them, which share its steps.  Sums of the waves are added in LDS
-// in a fixed order.  Measured (us, in a captured graph, the first product's launch included where there are adapters): one row 4096 -> 14336, r = 16, 12.2 (31 MB of weights; codes
-// from memory straight into the lanes that use them 22); 16 rows 4096 -> 6144, no adapters 6.2, 12 of r = 16 10.1; 16 rows 14336 -> 4096 11.8 and 17.2.  Three blocks
+// in a fixed order.  Measured (us, in a captured graph, the first product's launch included where there are adapters): one row 4096 -> 14336, r = 16, 12.2 (31 MB of weights; without adapters 8.4; codes
+// from memory straight into the lanes that use them 22); 16 rows 4096 -> 6144, no adapters 6.0, 12 of r = 16 10.1; 16 rows 14336 -> 4096 11.7 and 17.2.  Three blocks
 // to a ring of the 16 x 32 tiles instead of two, which is all that LDS holds: the same.
 template <int XC_, int NI_, int NW_, int TW_, int D_>
 struct FewLayer {
